@@ -38,6 +38,14 @@
  *   8. zarya_mdm_reveal       the positions revealed at a step, their tokens
  *                             written and their mask flags cleared.
  *
+ * A prefix cache that stays small while sequences grow (both compose):
+ *
+ *   9. zarya_slot_attn_window  attention over a sliding window of the prefix,
+ *                              with the first places kept (sinks);
+ *  10. zarya_kv_quantize, zarya_kv_dequantize, zarya_kv_append_q4
+ *                              a cache held in 4 bits;
+ *  11. zarya_slot_attn_q4      attention over that cache.
+ *
  * Conventions for every entry point:
  *  - Tensor arguments are DEVICE pointers to dense row-major (C-contiguous)
  *    arrays whose shapes are given in the comments; the caller owns every
@@ -439,6 +447,130 @@ typedef enum zarya_reveal_rule {
 zarya_status zarya_mdm_reveal(int32_t batch, int32_t n, const float* conf, uint8_t* mask, const int32_t* k,
                               int32_t rule, uint64_t seed, uint64_t offset, const int32_t* sample_id, int32_t* tokens,
                               int32_t* order, int32_t* n_revealed, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* 9. Slot attention over a window of the prefix, with sinks                 */
+/* ------------------------------------------------------------------------ */
+/*
+ * zarya_slot_attn for models with sliding-window layers, and for serving long
+ * sequences with a bounded cost a step.  Places are counted in the committed
+ * order: prefix row j has place j and draft token t the place P_b + t.  A key
+ * that zarya_slot_attn shows to a token at place i is seen when its place j has
+ *   j < sinks   or   j > i - window,
+ * draft tokens' keys included (a token always sees itself, and in the DIFFUSION
+ * pass the later tokens of its slot).  Keys that no token of a call sees are not
+ * read.  A window of P_b + T or more changes nothing.
+ */
+typedef struct zarya_attn_window {
+  int32_t window; /* >= 1: keys that a token sees, itself among them, besides the sinks */
+  int32_t sinks;  /* >= 0: first places that stay visible                              */
+} zarya_attn_window;
+
+/* Bytes of device workspace zarya_slot_attn_window needs (may be 0).  With
+ * prefix_splits = 0 the size for the longest prefix_len of a call serves every
+ * shorter one. */
+zarya_status zarya_slot_attn_window_workspace_size(const zarya_slot_attn_desc* desc, const zarya_attn_window* window,
+                                                   size_t* bytes);
+
+/*
+ * Arguments and results as zarya_slot_attn's.  q, the caches, the slot K/V, out
+ * and the workspace must be 16-byte aligned.  A value that a row does not see
+ * never reaches it, infinities and NaN included.
+ * ZARYA_ERR_UNSUPPORTED as zarya_slot_attn, and where prefix_len + T is 2^31 - 64
+ * or more.
+ */
+zarya_status zarya_slot_attn_window(const zarya_slot_attn_desc* desc, const zarya_attn_window* window, const void* q,
+                                    const void* k_cache, const void* v_cache, const void* k_slot, const void* v_slot,
+                                    const uint8_t* slot_pass, const int32_t* prefix_lens, void* out, float* lse,
+                                    void* workspace, size_t workspace_bytes, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* 10. The 4-bit cache                                                       */
+/* ------------------------------------------------------------------------ */
+/*
+ * K and V of the prefix in 4 bits an element and a scale byte per 32: 136 bytes
+ * a row of K and V at D = 128 instead of 512.  Each of the two is held in
+ *   codes  [B, Hkv, C, D/2]  uint8   element 2i of a row in the low bits of byte i,
+ *                                    element 2i + 1 in the high bits
+ *   scales [B, Hkv, C, D/32] uint8   one per block of 32 neighbouring elements
+ * A code is a sign (bit 3) and a magnitude (bits 0-2) of 0, 1/2, 1, 3/2, 2, 3, 4 or
+ * 6 (e2m1); an element's value is that times 2^(scale - 127).  A scale of 255
+ * marks a block that has no values: its elements read as NaN.  (These are the
+ * element and scale formats of the OCP Microscaling specification, MXFP4.)
+ * Codes and scales of any content are read by the same rule: a value beyond the
+ * range of bf16 and float32 reads as an infinity.
+ *
+ * Quantizing takes the smallest scale for which the block's largest magnitude
+ * rounds to at most 6, and rounds each element to the nearest magnitude, halves
+ * to the even code: no element is off by more than half a step.  (The scale is
+ * held to 252, the last for which 6 is finite; from 7 * 2^125 on a magnitude
+ * becomes 6 * 2^125.)  A block with a NaN or an infinity gets the scale 255.
+ * Values read back the same in bf16 and in float32 (both hold them exactly).
+ */
+typedef struct zarya_kv_q4_desc {
+  int32_t batch;       /* B >= 1                                     */
+  int32_t n_kv_heads;  /* Hkv >= 1                                   */
+  int32_t head_dim;    /* D: 64 or 128                               */
+  int32_t kv_capacity; /* C: row count of the cache arrays           */
+  int32_t n_rows;      /* N: row count of k and v, 0 <= N <= C       */
+  int32_t dtype;       /* zarya_dtype of k and v                     */
+} zarya_kv_q4_desc;
+
+/*
+ * A prefix (a prompt's keys and values) into the cache: rows n < lens[b] of batch
+ * row b are quantized into the cache rows starts[b] + n.
+ *
+ * k, v    [B, Hkv, N, D] dtype
+ * starts  [B] int32 or NULL (0)
+ * lens    [B] int32 or NULL (N); values are clamped to [0, N]
+ * A batch row with a negative start, or whose rows would pass C, is left
+ * unchanged (checked on the GPU); so is every other row of the cache.  k, v and
+ * the codes must be 16-byte aligned and must not overlap.
+ * ZARYA_ERR_UNSUPPORTED: head_dim not 64 or 128; B*Hkv*C at or above 2^31.
+ */
+zarya_status zarya_kv_quantize(const zarya_kv_q4_desc* desc, const void* k, const void* v, const int32_t* starts,
+                               const int32_t* lens, uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes,
+                               uint8_t* v_scales, hipStream_t stream);
+
+/*
+ * The values of cache rows n < lens[b] into k and v ([B, Hkv, N, D] dtype); rows
+ * from lens[b] on are left as they were.  Requirements as above.
+ */
+zarya_status zarya_kv_dequantize(const zarya_kv_q4_desc* desc, const uint8_t* k_codes, const uint8_t* k_scales,
+                                 const uint8_t* v_codes, const uint8_t* v_scales, const int32_t* lens, void* k, void* v,
+                                 hipStream_t stream);
+
+/*
+ * zarya_kv_append into the 4-bit cache: the accepted tokens' K/V are quantized as
+ * they are appended.  Everything else, rows that do not fit included, is as
+ * there.  The slot K/V and the codes must be 16-byte aligned.
+ */
+zarya_status zarya_kv_append_q4(const zarya_kv_append_desc* desc, const void* k_slot, const void* v_slot,
+                                const uint8_t* accepted, const int32_t* order, int32_t* prefix_lens, uint8_t* k_codes,
+                                uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, hipStream_t stream);
+
+/* ------------------------------------------------------------------------ */
+/* 11. Slot attention over the 4-bit cache                                   */
+/* ------------------------------------------------------------------------ */
+/*
+ * zarya_slot_attn with the prefix read from a 4-bit cache (the draft tokens' own
+ * K/V are of the call's dtype), over the whole prefix or, with `window`, over a
+ * window of it with sinks (as zarya_slot_attn_window; NULL or a window of 0: the
+ * whole prefix).  The codes are multiplied as the values they stand for: results
+ * are those of zarya_slot_attn over the dequantized cache, to rounding.
+ */
+zarya_status zarya_slot_attn_q4_workspace_size(const zarya_slot_attn_desc* desc, const zarya_attn_window* window,
+                                               size_t* bytes);
+
+/*
+ * The cache arrays may be NULL only when P == 0.  q, the codes, the slot K/V, out
+ * and the workspace must be 16-byte aligned.  The rest as zarya_slot_attn_window.
+ */
+zarya_status zarya_slot_attn_q4(const zarya_slot_attn_desc* desc, const zarya_attn_window* window, const void* q,
+                                const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,
+                                const uint8_t* v_scales, const void* k_slot, const void* v_slot,
+                                const uint8_t* slot_pass, const int32_t* prefix_lens, void* out, float* lse,
+                                void* workspace, size_t workspace_bytes, hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
 /* Diagnostics                                                               */

@@ -52,6 +52,7 @@ from .selection import (
 from .sampling import gumbel, philox4x32, slot_sample, uniforms
 from .verify import ACCEPT_PREFIX, ACCEPT_PER_TOKEN, accept_tokens, kv_append
 from .mdm import REVEAL_CONFIDENCE, REVEAL_LEFTMOST, REVEAL_RANDOM, mask_budget, reveal
+from .view import q4_dequantize, q4_quantize, view_attention, window_visibility
 
 __all__ = [
     "PASS_DIFFUSION",
@@ -83,4 +84,8 @@ __all__ = [
     "REVEAL_RANDOM",
     "mask_budget",
     "reveal",
+    "window_visibility",
+    "view_attention",
+    "q4_quantize",
+    "q4_dequantize",
 ]

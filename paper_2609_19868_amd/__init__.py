@@ -13,6 +13,12 @@ update"):
 * :func:`verify_accept`    -- accepted tokens of the verified slots
 * :func:`kv_append`        -- the accepted tokens' K/V appended to the cache
 
+A prefix cache that stays small while sequences grow (both compose):
+
+* :func:`slot_attn` with ``window`` and ``sinks`` -- a sliding window of the prefix
+* :class:`Q4Cache`, :func:`kv_quantize`, :func:`kv_dequantize`,
+  :func:`kv_append_q4`, :func:`slot_attn_q4` -- a cache held in 4 bits
+
 Each function marshals torch tensors (device memory) and torch's current
 stream into the C ABI of ``include/zarya.h``; all arithmetic runs in the HIP
 kernels.  Outputs and workspaces are allocated with torch unless passed in.
@@ -22,6 +28,7 @@ from __future__ import annotations
 
 import ctypes
 import math
+from typing import NamedTuple
 
 import torch
 
@@ -58,6 +65,12 @@ __all__ = [
     "select_slots",
     "verify_accept",
     "kv_append",
+    "Q4Cache",
+    "q4_cache",
+    "kv_quantize",
+    "kv_dequantize",
+    "kv_append_q4",
+    "slot_attn_q4",
     "ZaryaError",
     "ACCEPT_PREFIX",
     "ACCEPT_PER_TOKEN",
@@ -149,13 +162,17 @@ def slot_attn_desc(q, k_cache, k_slot, n_slots, slot_len, pass_=PASS_DIFFUSION, 
 
 def slot_attn(q, k_cache, v_cache, k_slot, v_slot, n_slots, slot_len, pass_=PASS_DIFFUSION,
               cross_slot=CROSS_SLOT_NONE, slot_pass=None, prefix_len=None, softmax_scale=None,
-              out=None, lse=None, want_lse=True, workspace=None, prefix_splits=0, prefix_lens=None):
+              out=None, lse=None, want_lse=True, workspace=None, prefix_splits=0, prefix_lens=None,
+              window=None, sinks=0):
     """Attention of S draft slots x L tokens against a prefix KV cache.
 
     q [B,Hq,T,D], k_cache/v_cache [B,Hkv,C,D] (or None when there is no
     prefix), k_slot/v_slot [B,Hkv,T,D], slot_pass [B,S] uint8 or None,
     prefix_lens [B] int32 per-row prefix lengths (each at most prefix_len,
     which defaults to C) or None.
+    window, sinks: a key at place j of the committed order (the prefix, then the
+    draft tokens) is seen from place i only when j > i - window or j < sinks
+    (window >= 1; None: no window, and sinks must be 0).
     Returns (out [B,Hq,T,D], lse [B,Hq,T] float32 or None).
     """
     B, Hq, T, D = q.shape
@@ -180,12 +197,101 @@ def slot_attn(q, k_cache, v_cache, k_slot, v_slot, n_slots, slot_len, pass_=PASS
         lse = torch.empty((B, Hq, T), dtype=torch.float32, device=dev)
     if lse is not None:
         _need(lse, "lse", (B, Hq, T), torch.float32, dev)
-    ws_bytes = _lib.slot_attn_workspace_size(desc)
+    win = _window(window, sinks)
+    ws_bytes = _lib.slot_attn_workspace_size(desc) if win is None else _lib.slot_attn_window_workspace_size(desc, win)
     _need_workspace(workspace, ws_bytes, dev)
     if workspace is None and ws_bytes > 0:
         workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
-    _call(_lib.lib().zarya_slot_attn, dev, ctypes.byref(desc), _ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_slot),
-          _ptr(v_slot), _ptr(slot_pass), _ptr(prefix_lens), _ptr(out), _ptr(lse), _ptr(workspace),
+    args = (_ptr(q), _ptr(k_cache), _ptr(v_cache), _ptr(k_slot), _ptr(v_slot), _ptr(slot_pass), _ptr(prefix_lens),
+            _ptr(out), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel())
+    if win is None:
+        _call(_lib.lib().zarya_slot_attn, dev, ctypes.byref(desc), *args)
+    else:
+        _call(_lib.lib().zarya_slot_attn_window, dev, ctypes.byref(desc), ctypes.byref(win), *args)
+    return out, lse
+
+
+class Q4Cache(NamedTuple):
+    """A prefix cache in 4 bits: codes [B,Hkv,C,D/2] and scales [B,Hkv,C,D/32],
+    all uint8 (the format is in ``include/zarya.h``)."""
+
+    k: torch.Tensor
+    k_scale: torch.Tensor
+    v: torch.Tensor
+    v_scale: torch.Tensor
+
+
+def q4_cache(batch, n_kv_heads, capacity, head_dim, device="cuda"):
+    """A :class:`Q4Cache` of ``capacity`` rows a head, all of them zeros."""
+    def zeros(n):
+        return torch.zeros((batch, n_kv_heads, capacity, n), dtype=torch.uint8, device=device)
+
+    return Q4Cache(zeros(head_dim // 2), zeros(head_dim // 32), zeros(head_dim // 2), zeros(head_dim // 32))
+
+
+def _need_q4(cache, device):
+    """(B, Hkv, C, D) of a cache whose four arrays fit together and are on `device`."""
+    if cache.k.dim() != 4:
+        raise ValueError(f"cache.k: expected 4 dimensions, got {tuple(cache.k.shape)}")
+    B, Hkv, C, half = cache.k.shape
+    _need(cache.k, "cache.k", (B, Hkv, C, half), torch.uint8, device)
+    _need(cache.v, "cache.v", (B, Hkv, C, half), torch.uint8, device)
+    _need(cache.k_scale, "cache.k_scale", (B, Hkv, C, half // 16), torch.uint8, device)
+    _need(cache.v_scale, "cache.v_scale", (B, Hkv, C, half // 16), torch.uint8, device)
+    return B, Hkv, C, 2 * half
+
+
+def _window(window, sinks):
+    if window is None:
+        if sinks:
+            raise ValueError("sinks need a window")
+        return None
+    return _lib.AttnWindow(window=_int32(window, "window"), sinks=_int32(sinks, "sinks"))
+
+
+def _int32(x, name):
+    # ctypes would cut a larger number to its low 32 bits
+    if not -(2**31) <= int(x) < 2**31:
+        raise ValueError(f"{name}: {x} does not fit 32 bits")
+    return int(x)
+
+
+def slot_attn_q4(q, cache, k_slot, v_slot, n_slots, slot_len, pass_=PASS_DIFFUSION, cross_slot=CROSS_SLOT_NONE,
+                 slot_pass=None, prefix_len=None, softmax_scale=None, out=None, lse=None, want_lse=True,
+                 workspace=None, prefix_splits=0, prefix_lens=None, window=None, sinks=0):
+    """:func:`slot_attn` over a prefix held in 4 bits (a :class:`Q4Cache`).
+
+    q, k_slot and v_slot are bf16 or float32.  The codes are multiplied as the
+    values they stand for; the other arguments and the results are those of
+    :func:`slot_attn`.
+    """
+    B, Hq, T, D = q.shape
+    dev, dt = q.device, q.dtype
+    Hkv = k_slot.shape[1]
+    desc = slot_attn_desc(q, cache.k, k_slot, n_slots, slot_len, pass_, cross_slot, prefix_len, softmax_scale,
+                          prefix_splits)
+    _need(q, "q", (B, Hq, T, D), dt, dev)
+    _need(k_slot, "k_slot", (B, Hkv, T, D), dt, dev)
+    _need(v_slot, "v_slot", (B, Hkv, T, D), dt, dev)
+    shape = _need_q4(cache, dev)
+    if shape != (B, Hkv, desc.kv_capacity, D):
+        raise ValueError(f"cache: expected batch, heads and head size {(B, Hkv, D)}, got {(shape[0], shape[1], shape[3])}")
+    _need_opt(slot_pass, "slot_pass", (B, n_slots), torch.uint8, dev)
+    _need_opt(prefix_lens, "prefix_lens", (B,), torch.int32, dev)
+    if out is None:
+        out = torch.empty((B, Hq, T, D), dtype=dt, device=dev)
+    _need(out, "out", (B, Hq, T, D), dt, dev)
+    if lse is None and want_lse:
+        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=dev)
+    _need_opt(lse, "lse", (B, Hq, T), torch.float32, dev)
+    win = _window(window, sinks)
+    ws_bytes = _lib.slot_attn_q4_workspace_size(desc, win)
+    _need_workspace(workspace, ws_bytes, dev)
+    if workspace is None and ws_bytes > 0:
+        workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
+    _call(_lib.lib().zarya_slot_attn_q4, dev, ctypes.byref(desc), None if win is None else ctypes.byref(win), _ptr(q),
+          _ptr(cache.k), _ptr(cache.k_scale), _ptr(cache.v), _ptr(cache.v_scale), _ptr(k_slot), _ptr(v_slot),
+          _ptr(slot_pass), _ptr(prefix_lens), _ptr(out), _ptr(lse), _ptr(workspace),
           0 if workspace is None else workspace.numel())
     return out, lse
 
@@ -381,3 +487,74 @@ def kv_append(k_cache, v_cache, prefix_lens, k_slot, v_slot, accepted, order):
     _call(_lib.lib().zarya_kv_append, dev, ctypes.byref(desc), _ptr(k_slot), _ptr(v_slot), _ptr(accepted),
           _ptr(order), _ptr(prefix_lens), _ptr(k_cache), _ptr(v_cache))
     return k_cache, v_cache, prefix_lens
+
+
+def kv_quantize(k, v, cache, starts=None, lens=None):
+    """Quantize keys and values into a 4-bit cache, in place.
+
+    k, v [B,Hkv,N,D] (bf16 or float32): rows n < lens[b] (int32 [B]; default N)
+    become cache rows starts[b] + n (int32 [B]; default 0).  A batch row that
+    would pass the capacity is left unchanged.  Returns the cache.
+    """
+    dev, dt = k.device, k.dtype
+    B, Hkv, C, D = _need_q4(cache, dev)
+    N = k.shape[2]
+    if dt not in _DT:
+        raise ValueError(f"unsupported dtype {dt}")
+    _need(k, "k", (B, Hkv, N, D), dt, dev)
+    _need(v, "v", (B, Hkv, N, D), dt, dev)
+    _need_opt(starts, "starts", (B,), torch.int32, dev)
+    _need_opt(lens, "lens", (B,), torch.int32, dev)
+    desc = _lib.KvQ4Desc(batch=B, n_kv_heads=Hkv, head_dim=D, kv_capacity=C, n_rows=N, dtype=_DT[dt])
+    _call(_lib.lib().zarya_kv_quantize, dev, ctypes.byref(desc), _ptr(k), _ptr(v), _ptr(starts), _ptr(lens),
+          _ptr(cache.k), _ptr(cache.k_scale), _ptr(cache.v), _ptr(cache.v_scale))
+    return cache
+
+
+def kv_dequantize(cache, n_rows=None, dtype=torch.bfloat16, lens=None, out=None):
+    """The values of a 4-bit cache's first n_rows rows (default: all of them).
+
+    lens: int32 [B] or None; rows from lens[b] on are left as they are in ``out``
+    (unset where the call makes its own).  Returns (k, v) [B,Hkv,n_rows,D].
+    """
+    dev = cache.k.device
+    B, Hkv, C, D = _need_q4(cache, dev)
+    N = C if n_rows is None else int(n_rows)
+    if dtype not in _DT:
+        raise ValueError(f"unsupported dtype {dtype}")
+    if not 0 <= N <= C:
+        raise ValueError(f"n_rows: {N} is not in [0, {C}]")
+    _need_opt(lens, "lens", (B,), torch.int32, dev)
+    if out is None:
+        out = tuple(torch.empty((B, Hkv, N, D), dtype=dtype, device=dev) for _ in range(2))
+    k, v = out
+    _need(k, "out[0] (k)", (B, Hkv, N, D), dtype, dev)
+    _need(v, "out[1] (v)", (B, Hkv, N, D), dtype, dev)
+    desc = _lib.KvQ4Desc(batch=B, n_kv_heads=Hkv, head_dim=D, kv_capacity=C, n_rows=N, dtype=_DT[dtype])
+    _call(_lib.lib().zarya_kv_dequantize, dev, ctypes.byref(desc), _ptr(cache.k), _ptr(cache.k_scale), _ptr(cache.v),
+          _ptr(cache.v_scale), _ptr(lens), _ptr(k), _ptr(v))
+    return k, v
+
+
+def kv_append_q4(cache, prefix_lens, k_slot, v_slot, accepted, order):
+    """:func:`kv_append` into a 4-bit cache: the accepted tokens' K/V are quantized
+    as they are appended, in place, and prefix_lens [B] int32 grows.
+
+    k_slot/v_slot [B,Hkv,S*L,D] (bf16 or float32), accepted [B,S,L] uint8, order
+    [B,S] int32 (slots in append order, the first -1 ends it).
+    """
+    dev, dt = k_slot.device, k_slot.dtype
+    B, Hkv, C, D = _need_q4(cache, dev)
+    _, S, L = accepted.shape
+    if dt not in _DT:
+        raise ValueError(f"unsupported dtype {dt}")
+    _need(k_slot, "k_slot", (B, Hkv, S * L, D), dt, dev)
+    _need(v_slot, "v_slot", (B, Hkv, S * L, D), dt, dev)
+    _need(accepted, "accepted", (B, S, L), torch.uint8, dev)
+    _need(order, "order", (B, S), torch.int32, dev)
+    _need(prefix_lens, "prefix_lens", (B,), torch.int32, dev)
+    desc = _lib.KvAppendDesc(batch=B, n_kv_heads=Hkv, head_dim=D, kv_capacity=C, n_slots=S, slot_len=L,
+                             dtype=_DT[dt])
+    _call(_lib.lib().zarya_kv_append_q4, dev, ctypes.byref(desc), _ptr(k_slot), _ptr(v_slot), _ptr(accepted),
+          _ptr(order), _ptr(prefix_lens), _ptr(cache.k), _ptr(cache.k_scale), _ptr(cache.v), _ptr(cache.v_scale))
+    return cache, prefix_lens

@@ -51,6 +51,13 @@ EXPORTS = (
     "zarya_slot_sample",
     "zarya_mdm_budget",
     "zarya_mdm_reveal",
+    "zarya_slot_attn_window_workspace_size",
+    "zarya_slot_attn_window",
+    "zarya_kv_quantize",
+    "zarya_kv_dequantize",
+    "zarya_kv_append_q4",
+    "zarya_slot_attn_q4_workspace_size",
+    "zarya_slot_attn_q4",
     "zarya_status_string",
     "zarya_last_error",
     "zarya_version",
@@ -113,6 +120,24 @@ class KvAppendDesc(ctypes.Structure):
     ]
 
 
+class AttnWindow(ctypes.Structure):
+    _fields_ = [
+        ("window", ctypes.c_int32),
+        ("sinks", ctypes.c_int32),
+    ]
+
+
+class KvQ4Desc(ctypes.Structure):
+    _fields_ = [
+        ("batch", ctypes.c_int32),
+        ("n_kv_heads", ctypes.c_int32),
+        ("head_dim", ctypes.c_int32),
+        ("kv_capacity", ctypes.c_int32),
+        ("n_rows", ctypes.c_int32),
+        ("dtype", ctypes.c_int32),
+    ]
+
+
 class ZaryaError(RuntimeError):
     def __init__(self, status, message):
         super().__init__(f"{status_name(status)}: {message}")
@@ -161,6 +186,22 @@ def lib():
         L.zarya_mdm_budget.restype = ctypes.c_int
         L.zarya_mdm_reveal.argtypes = [i32, i32, vp, vp, vp, i32, u64, u64, vp, vp, vp, vp, vp]
         L.zarya_mdm_reveal.restype = ctypes.c_int
+        view_size = [ctypes.POINTER(SlotAttnDesc), ctypes.POINTER(AttnWindow), ctypes.POINTER(sz)]
+        L.zarya_slot_attn_window_workspace_size.argtypes = view_size
+        L.zarya_slot_attn_window_workspace_size.restype = ctypes.c_int
+        L.zarya_slot_attn_window.argtypes = [ctypes.POINTER(SlotAttnDesc), ctypes.POINTER(AttnWindow)] + [vp] * 10 + [
+            sz, vp]
+        L.zarya_slot_attn_window.restype = ctypes.c_int
+        L.zarya_slot_attn_q4_workspace_size.argtypes = view_size
+        L.zarya_slot_attn_q4_workspace_size.restype = ctypes.c_int
+        L.zarya_slot_attn_q4.argtypes = [ctypes.POINTER(SlotAttnDesc), ctypes.POINTER(AttnWindow)] + [vp] * 12 + [sz, vp]
+        L.zarya_slot_attn_q4.restype = ctypes.c_int
+        L.zarya_kv_quantize.argtypes = [ctypes.POINTER(KvQ4Desc)] + [vp] * 9
+        L.zarya_kv_quantize.restype = ctypes.c_int
+        L.zarya_kv_dequantize.argtypes = [ctypes.POINTER(KvQ4Desc)] + [vp] * 8
+        L.zarya_kv_dequantize.restype = ctypes.c_int
+        L.zarya_kv_append_q4.argtypes = [ctypes.POINTER(KvAppendDesc)] + [vp] * 10
+        L.zarya_kv_append_q4.restype = ctypes.c_int
         L.zarya_status_string.argtypes = [ctypes.c_int]
         L.zarya_status_string.restype = ctypes.c_char_p
         L.zarya_last_error.argtypes = []
@@ -202,4 +243,17 @@ def slot_confidence_workspace_size(desc: ConfDesc) -> int:
 def slot_sample_workspace_size(desc: ConfDesc) -> int:
     n = ctypes.c_size_t(0)
     check(lib().zarya_slot_sample_workspace_size(ctypes.byref(desc), ctypes.byref(n)))
+    return n.value
+
+
+def slot_attn_window_workspace_size(desc: SlotAttnDesc, window: AttnWindow) -> int:
+    n = ctypes.c_size_t(0)
+    check(lib().zarya_slot_attn_window_workspace_size(ctypes.byref(desc), ctypes.byref(window), ctypes.byref(n)))
+    return n.value
+
+
+def slot_attn_q4_workspace_size(desc: SlotAttnDesc, window: AttnWindow | None = None) -> int:
+    n = ctypes.c_size_t(0)
+    w = None if window is None else ctypes.byref(window)
+    check(lib().zarya_slot_attn_q4_workspace_size(ctypes.byref(desc), w, ctypes.byref(n)))
     return n.value

@@ -10,6 +10,7 @@
 #include <mutex>
 #include <string>
 
+#include "host.hpp"
 #include "kernels.hpp"
 #include "zarya.h"
 
@@ -22,8 +23,10 @@ using namespace zarya;
 static __device__ __align__(256) uint8_t scratch[kConfScratchBytes];
 
 namespace {
-
 thread_local std::string g_last_error;
+}
+
+namespace zarya {
 
 zarya_status fail(zarya_status st, const char* fmt, ...) {
   char buf[512];
@@ -39,19 +42,6 @@ zarya_status hip_status(hipError_t e, const char* what) {
   if (e == hipSuccess) return ZARYA_OK;
   return fail(ZARYA_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
 }
-
-constexpr int64_t kI32Max = 2147483647;
-
-size_t align256(size_t x) { return (x + 255) & ~(size_t)255; }
-
-// ------------------------------------------------------------- attention plan
-
-struct AttnPlan {
-  int T, G, R;
-  int n_split, tiles_per_split, n_prefix_tiles, n_rb, rows_per_block;
-  int64_t rows_total;
-  size_t ws_bytes;
-};
 
 zarya_status check_attn_desc(const zarya_slot_attn_desc* d) {
   if (!d) return fail(ZARYA_ERR_INVALID_ARGUMENT, "desc is NULL");
@@ -83,6 +73,37 @@ zarya_status check_attn_desc(const zarya_slot_attn_desc* d) {
     return fail(ZARYA_ERR_UNSUPPORTED, "problem too large: batch*heads*tokens must stay below 2^31");
   return ZARYA_OK;
 }
+
+zarya_status check_append_desc(const zarya_kv_append_desc* d) {
+  if (!d) return fail(ZARYA_ERR_INVALID_ARGUMENT, "desc is NULL");
+  if (d->batch < 1 || d->batch > 65535) return fail(ZARYA_ERR_INVALID_ARGUMENT, "batch must be in [1, 65535]");
+  if (d->n_kv_heads < 1 || d->n_slots < 1 || d->slot_len < 1 || d->kv_capacity < 0)
+    return fail(ZARYA_ERR_INVALID_ARGUMENT, "n_kv_heads, n_slots and slot_len must be >= 1, kv_capacity >= 0");
+  if (d->dtype != ZARYA_DTYPE_F32 && d->dtype != ZARYA_DTYPE_BF16)
+    return fail(ZARYA_ERR_INVALID_ARGUMENT, "unknown dtype %d", d->dtype);
+  if (d->head_dim != 64 && d->head_dim != 128)
+    return fail(ZARYA_ERR_UNSUPPORTED, "head_dim %d is not supported (64 or 128)", d->head_dim);
+  if (d->n_slots > 1024) return fail(ZARYA_ERR_UNSUPPORTED, "n_slots %d exceeds 1024", d->n_slots);
+  if ((int64_t)d->n_slots * d->slot_len > kAppendMaxTokens)
+    return fail(ZARYA_ERR_UNSUPPORTED, "n_slots * slot_len exceeds %d", kAppendMaxTokens);
+  if ((int64_t)d->batch * d->n_kv_heads * std::max<int64_t>(d->kv_capacity, (int64_t)d->n_slots * d->slot_len) >
+      kI32Max)
+    return fail(ZARYA_ERR_UNSUPPORTED, "problem too large: batch*heads*tokens must stay below 2^31");
+  return ZARYA_OK;
+}
+
+}  // namespace zarya
+
+namespace {
+
+// ------------------------------------------------------------- attention plan
+
+struct AttnPlan {
+  int T, G, R;
+  int n_split, tiles_per_split, n_prefix_tiles, n_rb, rows_per_block;
+  int64_t rows_total;
+  size_t ws_bytes;
+};
 
 AttnPlan plan_attn(const zarya_slot_attn_desc* d) {
   AttnPlan pl{};
@@ -679,20 +700,8 @@ zarya_status zarya_verify_accept(int32_t batch, int32_t n_slots, int32_t slot_le
 zarya_status zarya_kv_append(const zarya_kv_append_desc* d, const void* k_slot, const void* v_slot,
                              const uint8_t* accepted, const int32_t* order, int32_t* prefix_lens, void* k_cache,
                              void* v_cache, hipStream_t stream) {
-  if (!d) return fail(ZARYA_ERR_INVALID_ARGUMENT, "desc is NULL");
-  if (d->batch < 1 || d->batch > 65535) return fail(ZARYA_ERR_INVALID_ARGUMENT, "batch must be in [1, 65535]");
-  if (d->n_kv_heads < 1 || d->n_slots < 1 || d->slot_len < 1 || d->kv_capacity < 0)
-    return fail(ZARYA_ERR_INVALID_ARGUMENT, "n_kv_heads, n_slots and slot_len must be >= 1, kv_capacity >= 0");
-  if (d->dtype != ZARYA_DTYPE_F32 && d->dtype != ZARYA_DTYPE_BF16)
-    return fail(ZARYA_ERR_INVALID_ARGUMENT, "unknown dtype %d", d->dtype);
-  if (d->head_dim != 64 && d->head_dim != 128)
-    return fail(ZARYA_ERR_UNSUPPORTED, "head_dim %d is not supported (64 or 128)", d->head_dim);
-  if (d->n_slots > 1024) return fail(ZARYA_ERR_UNSUPPORTED, "n_slots %d exceeds 1024", d->n_slots);
-  if ((int64_t)d->n_slots * d->slot_len > kAppendMaxTokens)
-    return fail(ZARYA_ERR_UNSUPPORTED, "n_slots * slot_len exceeds %d", kAppendMaxTokens);
-  if ((int64_t)d->batch * d->n_kv_heads * std::max<int64_t>(d->kv_capacity, (int64_t)d->n_slots * d->slot_len) >
-      kI32Max)
-    return fail(ZARYA_ERR_UNSUPPORTED, "problem too large: batch*heads*tokens must stay below 2^31");
+  const zarya_status st = check_append_desc(d);
+  if (st != ZARYA_OK) return st;
   if (!k_slot || !v_slot || !accepted || !order || !prefix_lens || !k_cache || !v_cache)
     return fail(ZARYA_ERR_INVALID_ARGUMENT, "every tensor argument is required");
   (void)hipGetLastError();

@@ -1,0 +1,287 @@
+// Host side of the entry points over a bounded view of the prefix cache: a window
+// with sinks, and the 4-bit cache.  Validation, work decomposition and launches,
+// as in api.hip.
+#include <algorithm>
+
+#include "host.hpp"
+#include "kernels.hpp"
+#include "zarya.h"
+
+using namespace zarya;
+
+namespace {
+
+struct ViewPlan {
+  int T, G, R;
+  int rows_per_block, n_rb, n_split;
+  int64_t rows_total, items;
+  size_t ws_o, ws_bytes;  // bytes of the partial outputs; of the whole workspace
+};
+
+int window_of(const zarya_attn_window* w) { return w && w->window > 0 ? w->window : (int)kI32Max; }
+int sinks_of(const zarya_attn_window* w) { return w && w->window > 0 ? w->sinks : 0; }
+
+zarya_status check_view(const zarya_slot_attn_desc* d, const zarya_attn_window* w, bool window_required) {
+  const zarya_status st = check_attn_desc(d);
+  if (st != ZARYA_OK) return st;
+  if (window_required && !w) return fail(ZARYA_ERR_INVALID_ARGUMENT, "window is NULL");
+  if (w && (w->window < (window_required ? 1 : 0) || w->sinks < 0))
+    return fail(ZARYA_ERR_INVALID_ARGUMENT, "window (%d) must be >= %d and sinks (%d) >= 0", w->window,
+                window_required ? 1 : 0, w->sinks);
+  // places and the ends of key tiles are 32-bit numbers
+  if ((int64_t)d->prefix_len + (int64_t)d->n_slots * d->slot_len > kI32Max - kAttnKeysPerTile)
+    return fail(ZARYA_ERR_UNSUPPORTED, "prefix_len + n_slots * slot_len must stay below 2^31 - %d", kAttnKeysPerTile);
+  return ZARYA_OK;
+}
+
+ViewPlan plan_view(const zarya_slot_attn_desc* d, const zarya_attn_window* w) {
+  ViewPlan pl{};
+  pl.T = d->n_slots * d->slot_len;
+  pl.G = d->n_q_heads / d->n_kv_heads;
+  pl.R = pl.G * pl.T;
+  pl.rows_total = (int64_t)d->batch * d->n_q_heads * pl.T;
+  pl.n_split = 1;
+  if (d->dtype == ZARYA_DTYPE_F32) return pl;
+  const int64_t groups = (int64_t)d->batch * d->n_kv_heads;
+  // prefix keys that a row block sees at most, its own tokens' shift of the window aside
+  const int64_t seen = std::min<int64_t>(d->prefix_len, (int64_t)window_of(w) + sinks_of(w));
+  int64_t want;    // splits that fill the units
+  int64_t tiles;   // key tiles, and how many of them a split has to keep
+  if (pl.R <= kViewFewRows) {
+    pl.rows_per_block = pl.R <= 16 ? 16 : 32;
+    pl.n_rb = (pl.R + pl.rows_per_block - 1) / pl.rows_per_block;
+    want = kViewFewTargetWGs / (groups * pl.n_rb);
+    tiles = (seen + 31) / 32 / kViewFewMinTiles;
+  } else {
+    const int n_narrow = (pl.R + kAttnRowsPerBlock - 1) / kAttnRowsPerBlock;
+    const int n_wide = (pl.R + kAttnWideRowsPerBlock - 1) / kAttnWideRowsPerBlock;
+    const bool wide = 2 * n_wide <= n_narrow && seen >= pl.T;
+    pl.rows_per_block = wide ? kAttnWideRowsPerBlock : kAttnRowsPerBlock;
+    pl.n_rb = wide ? n_wide : n_narrow;
+    want = kAttnTargetWGs / (groups * pl.n_rb);
+    tiles = (seen + kAttnKeysPerTile - 1) / kAttnKeysPerTile / 4;
+  }
+  const int64_t ns = d->prefix_splits > 0 ? std::min<int64_t>(d->prefix_splits, std::max<int64_t>(1, (seen + 31) / 32))
+                                          : std::min(want, tiles);
+  pl.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(ns, 64));
+  pl.items = groups * pl.n_rb * pl.n_split;
+  if (pl.n_split > 1) {
+    pl.ws_o = align256((size_t)pl.n_split * pl.rows_total * d->head_dim * 4);
+    pl.ws_bytes = pl.ws_o + align256((size_t)pl.n_split * pl.rows_total * 4);
+  }
+  return pl;
+}
+
+zarya_status view_workspace_size(const zarya_slot_attn_desc* d, const zarya_attn_window* w, bool window_required,
+                                 size_t* bytes) {
+  if (!bytes) return fail(ZARYA_ERR_INVALID_ARGUMENT, "bytes is NULL");
+  const zarya_status st = check_view(d, w, window_required);
+  if (st != ZARYA_OK) return st;
+  *bytes = plan_view(d, w).ws_bytes;
+  return ZARYA_OK;
+}
+
+bool aligned16(std::initializer_list<const void*> ptrs) {
+  return std::all_of(ptrs.begin(), ptrs.end(), [](const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; });
+}
+
+template <class Params, class T>
+void set_common(Params& p, const zarya_slot_attn_desc* d, const zarya_attn_window* w, const ViewPlan& pl, const void* q,
+                const void* k_cache, const void* v_cache, const uint8_t* k_scale, const uint8_t* v_scale,
+                const void* k_slot, const void* v_slot, const uint8_t* slot_pass, const int32_t* prefix_lens, void* out,
+                float* lse) {
+  p.q = static_cast<const T*>(q);
+  p.k_cache = static_cast<const T*>(k_cache);
+  p.v_cache = static_cast<const T*>(v_cache);
+  p.k_slot = static_cast<const T*>(k_slot);
+  p.v_slot = static_cast<const T*>(v_slot);
+  p.slot_pass = slot_pass;
+  p.prefix_lens = prefix_lens;
+  p.out = static_cast<T*>(out);
+  p.lse = lse;
+  p.B = d->batch;
+  p.Hq = d->n_q_heads;
+  p.Hkv = d->n_kv_heads;
+  p.P = d->prefix_len;
+  p.C = d->kv_capacity;
+  p.S = d->n_slots;
+  p.L = d->slot_len;
+  p.T = pl.T;
+  p.G = pl.G;
+  p.pass = d->pass;
+  p.cross = d->cross_slot;
+  p.rows_total = (int)pl.rows_total;
+  p.k_scale = k_scale;
+  p.v_scale = v_scale;
+  p.window = window_of(w);
+  p.sinks = sinks_of(w);
+}
+
+// `codes`: k_cache and v_cache are 4-bit codes
+zarya_status run_view(const zarya_slot_attn_desc* d, const zarya_attn_window* w, bool codes, const void* q,
+                      const void* k_cache, const uint8_t* k_scale, const void* v_cache, const uint8_t* v_scale,
+                      const void* k_slot, const void* v_slot, const uint8_t* slot_pass, const int32_t* prefix_lens,
+                      void* out, float* lse, void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  if (!q || !k_slot || !v_slot || !out) return fail(ZARYA_ERR_INVALID_ARGUMENT, "q, k_slot, v_slot and out are required");
+  if (d->prefix_len > 0 && (!k_cache || !v_cache || (codes && (!k_scale || !v_scale))))
+    return fail(ZARYA_ERR_INVALID_ARGUMENT, "the cache arrays are required when prefix_len > 0");
+  if (!aligned16({q, k_cache, v_cache, k_slot, v_slot, out, workspace}))
+    return fail(ZARYA_ERR_INVALID_ARGUMENT, "q, the caches, the slot K/V, out and the workspace must be 16-byte aligned");
+  const ViewPlan pl = plan_view(d, w);
+  if (workspace_bytes < pl.ws_bytes)
+    return fail(ZARYA_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes is below the %zu required", workspace_bytes,
+                pl.ws_bytes);
+  if (pl.ws_bytes > 0 && !workspace) return fail(ZARYA_ERR_INVALID_ARGUMENT, "workspace is NULL");
+  (void)hipGetLastError();  // drop a stale error so the status below is ours
+
+  if (d->dtype == ZARYA_DTYPE_F32) {
+    ViewParams32 p{};
+    set_common<ViewParams32, float>(p, d, w, pl, q, k_cache, v_cache, k_scale, v_scale, k_slot, v_slot, slot_pass,
+                                    prefix_lens, out, lse);
+    p.scale = d->softmax_scale;
+    return hip_status(launch_slot_view_f32(p, d->head_dim, codes, stream), "slot attention view f32 launch");
+  }
+  if (pl.items > kI32Max / 2) return fail(ZARYA_ERR_UNSUPPORTED, "too many workgroups");
+  ViewParams p{};
+  set_common<ViewParams, uint16_t>(p, d, w, pl, q, k_cache, v_cache, k_scale, v_scale, k_slot, v_slot, slot_pass,
+                                   prefix_lens, out, lse);
+  if (pl.n_split > 1) {
+    p.part_o = static_cast<float*>(workspace);
+    p.part_lse = reinterpret_cast<float*>(static_cast<char*>(workspace) + pl.ws_o);
+  }
+  p.R = pl.R;
+  p.scale_log2 = d->softmax_scale * 1.4426950408889634f;
+  p.n_split = pl.n_split;
+  p.n_rb = pl.n_rb;
+  p.n_items = (int)pl.items;
+  p.per_xcd = (p.n_items + 7) / 8;
+  p.rows_per_block = pl.rows_per_block;
+  // as in zarya_slot_attn: under a causal order the row blocks with the most keys first
+  const bool few = pl.rows_per_block < kAttnRowsPerBlock;
+  const int64_t n_bg = (int64_t)d->batch * d->n_kv_heads;
+  p.heavy_first = !few && d->cross_slot == ZARYA_CROSS_SLOT_CAUSAL && pl.n_split == 1 && n_bg % 8 == 0 &&
+                  pl.items <= kAttnMaxGrid;
+  return hip_status(few ? launch_slot_view_few(p, d->head_dim, codes, stream)
+                        : launch_slot_view_bf16(p, d->head_dim, codes, stream),
+                    "slot attention view launch");
+}
+
+zarya_status check_q4_desc(const zarya_kv_q4_desc* d) {
+  if (!d) return fail(ZARYA_ERR_INVALID_ARGUMENT, "desc is NULL");
+  if (d->batch < 1 || d->n_kv_heads < 1 || d->n_rows < 0 || d->kv_capacity < 0)
+    return fail(ZARYA_ERR_INVALID_ARGUMENT, "batch and n_kv_heads must be >= 1, n_rows and kv_capacity >= 0");
+  if (d->dtype != ZARYA_DTYPE_F32 && d->dtype != ZARYA_DTYPE_BF16)
+    return fail(ZARYA_ERR_INVALID_ARGUMENT, "unknown dtype %d", d->dtype);
+  if (d->head_dim != 64 && d->head_dim != 128)
+    return fail(ZARYA_ERR_UNSUPPORTED, "head_dim %d is not supported (64 or 128)", d->head_dim);
+  if (d->n_rows > d->kv_capacity)
+    return fail(ZARYA_ERR_INVALID_ARGUMENT, "n_rows (%d) exceeds kv_capacity (%d)", d->n_rows, d->kv_capacity);
+  if ((int64_t)d->batch * d->n_kv_heads > kI32Max || (int64_t)d->batch * d->n_kv_heads * d->kv_capacity > kI32Max)
+    return fail(ZARYA_ERR_UNSUPPORTED, "problem too large: batch*heads*rows must stay below 2^31");
+  return ZARYA_OK;
+}
+
+zarya_status run_q4(bool quantize, const zarya_kv_q4_desc* d, const void* k, const void* v, const int32_t* starts,
+                    const int32_t* lens, Q4CachePtrs cache, hipStream_t stream) {
+  const zarya_status st = check_q4_desc(d);
+  if (st != ZARYA_OK) return st;
+  if (d->n_rows == 0) return ZARYA_OK;
+  if (!k || !v || !cache.k_codes || !cache.k_scales || !cache.v_codes || !cache.v_scales)
+    return fail(ZARYA_ERR_INVALID_ARGUMENT, "k, v and the four cache arrays are required");
+  if (!aligned16({k, v, cache.k_codes, cache.v_codes}))
+    return fail(ZARYA_ERR_INVALID_ARGUMENT, "k, v and the code arrays must be 16-byte aligned");
+  (void)hipGetLastError();
+  KvQ4Params p{};
+  p.B = d->batch;
+  p.Hkv = d->n_kv_heads;
+  p.C = d->kv_capacity;
+  p.N = d->n_rows;
+  p.D = d->head_dim;
+  p.bf16 = d->dtype == ZARYA_DTYPE_BF16;
+  p.k = const_cast<void*>(k);
+  p.v = const_cast<void*>(v);
+  p.starts = starts;
+  p.lens = lens;
+  p.cache = cache;
+  return hip_status(quantize ? launch_kv_quantize(p, stream) : launch_kv_dequantize(p, stream),
+                    quantize ? "kv_quantize launch" : "kv_dequantize launch");
+}
+
+}  // namespace
+
+extern "C" {
+
+zarya_status zarya_slot_attn_window_workspace_size(const zarya_slot_attn_desc* desc, const zarya_attn_window* window,
+                                                   size_t* bytes) {
+  return view_workspace_size(desc, window, true, bytes);
+}
+
+zarya_status zarya_slot_attn_window(const zarya_slot_attn_desc* desc, const zarya_attn_window* window, const void* q,
+                                    const void* k_cache, const void* v_cache, const void* k_slot, const void* v_slot,
+                                    const uint8_t* slot_pass, const int32_t* prefix_lens, void* out, float* lse,
+                                    void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  const zarya_status st = check_view(desc, window, true);
+  if (st != ZARYA_OK) return st;
+  return run_view(desc, window, false, q, k_cache, nullptr, v_cache, nullptr, k_slot, v_slot, slot_pass, prefix_lens, out,
+                  lse, workspace, workspace_bytes, stream);
+}
+
+zarya_status zarya_slot_attn_q4_workspace_size(const zarya_slot_attn_desc* desc, const zarya_attn_window* window,
+                                               size_t* bytes) {
+  return view_workspace_size(desc, window, false, bytes);
+}
+
+zarya_status zarya_slot_attn_q4(const zarya_slot_attn_desc* desc, const zarya_attn_window* window, const void* q,
+                                const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,
+                                const uint8_t* v_scales, const void* k_slot, const void* v_slot,
+                                const uint8_t* slot_pass, const int32_t* prefix_lens, void* out, float* lse,
+                                void* workspace, size_t workspace_bytes, hipStream_t stream) {
+  const zarya_status st = check_view(desc, window, false);
+  if (st != ZARYA_OK) return st;
+  return run_view(desc, window, true, q, k_codes, k_scales, v_codes, v_scales, k_slot, v_slot, slot_pass, prefix_lens,
+                  out, lse, workspace, workspace_bytes, stream);
+}
+
+zarya_status zarya_kv_quantize(const zarya_kv_q4_desc* desc, const void* k, const void* v, const int32_t* starts,
+                               const int32_t* lens, uint8_t* k_codes, uint8_t* k_scales, uint8_t* v_codes,
+                               uint8_t* v_scales, hipStream_t stream) {
+  return run_q4(true, desc, k, v, starts, lens, Q4CachePtrs{k_codes, k_scales, v_codes, v_scales}, stream);
+}
+
+zarya_status zarya_kv_dequantize(const zarya_kv_q4_desc* desc, const uint8_t* k_codes, const uint8_t* k_scales,
+                                 const uint8_t* v_codes, const uint8_t* v_scales, const int32_t* lens, void* k, void* v,
+                                 hipStream_t stream) {
+  return run_q4(false, desc, k, v, nullptr, lens,
+                Q4CachePtrs{const_cast<uint8_t*>(k_codes), const_cast<uint8_t*>(k_scales), const_cast<uint8_t*>(v_codes),
+                            const_cast<uint8_t*>(v_scales)},
+                stream);
+}
+
+zarya_status zarya_kv_append_q4(const zarya_kv_append_desc* d, const void* k_slot, const void* v_slot,
+                                const uint8_t* accepted, const int32_t* order, int32_t* prefix_lens, uint8_t* k_codes,
+                                uint8_t* k_scales, uint8_t* v_codes, uint8_t* v_scales, hipStream_t stream) {
+  const zarya_status st = check_append_desc(d);
+  if (st != ZARYA_OK) return st;
+  if (!k_slot || !v_slot || !accepted || !order || !prefix_lens || !k_codes || !k_scales || !v_codes || !v_scales)
+    return fail(ZARYA_ERR_INVALID_ARGUMENT, "every tensor argument is required");
+  if (!aligned16({k_slot, v_slot, k_codes, v_codes}))
+    return fail(ZARYA_ERR_INVALID_ARGUMENT, "the slot K/V and the code arrays must be 16-byte aligned");
+  (void)hipGetLastError();
+  AppendQ4Params p{};
+  p.B = d->batch;
+  p.Hkv = d->n_kv_heads;
+  p.C = d->kv_capacity;
+  p.S = d->n_slots;
+  p.L = d->slot_len;
+  p.k_slot = k_slot;
+  p.v_slot = v_slot;
+  p.accepted = accepted;
+  p.order = order;
+  p.prefix_lens = prefix_lens;
+  p.D = d->head_dim;
+  p.bf16 = d->dtype == ZARYA_DTYPE_BF16;
+  p.cache = Q4CachePtrs{k_codes, k_scales, v_codes, v_scales};
+  return hip_status(launch_kv_append_q4(p, stream), "kv_append_q4 launch");
+}
+
+}  // extern "C"

@@ -49,6 +49,19 @@ struct AttnParams32 {
   int item0;  // first work item of this launch (set by the launcher)
 };
 
+// The same over a bounded view of the prefix (attn_view.hpp).
+template <class Params>
+struct ViewOf : Params {
+  const uint8_t* k_scale;  // [B, Hkv, C, D/32] of 4-bit caches
+  const uint8_t* v_scale;
+  int window;  // >= 1 (INT32_MAX: none)
+  int sinks;
+};
+struct ViewParams : ViewOf<AttnParams> {
+  int item0;  // first work item of this launch (set by the launcher)
+};
+using ViewParams32 = ViewOf<AttnParams32>;
+
 // LM-head confidence.  Partials are per (vocab group, row): m = max logit,
 // s = sum of exp(logit - m), idx = lowest id at the max.
 struct ConfParams {
@@ -139,6 +152,29 @@ struct AppendParams {
   void* v_cache;
 };
 
+// The 4-bit cache: codes [B, Hkv, C, D/2] and scale bytes [B, Hkv, C, D/32] of K and V.
+struct Q4CachePtrs {
+  uint8_t* k_codes;
+  uint8_t* k_scales;
+  uint8_t* v_codes;
+  uint8_t* v_scales;
+};
+
+struct KvQ4Params {
+  int B, Hkv, C, N, D;
+  int bf16;
+  void* k;  // [B, Hkv, N, D], only read when quantizing
+  void* v;
+  const int32_t* starts;  // [B] or null
+  const int32_t* lens;    // [B] or null
+  Q4CachePtrs cache;      // only read when dequantizing
+};
+
+struct AppendQ4Params : AppendParams {
+  int D, bf16;
+  Q4CachePtrs cache;  // instead of k_cache and v_cache
+};
+
 // Mode A reveal: one workgroup per batch row sorts the row's N keys in LDS.
 struct RevealParams {
   int B, N, NP;  // NP = N rounded up to a power of two (>= 2)
@@ -170,6 +206,11 @@ constexpr int kAttnMaxGrid = 1 << 20;
 constexpr int kAttnRowsPerBlock = 128;      // four waves
 constexpr int kAttnWideRowsPerBlock = 256;  // eight waves: every K/V tile staged once for 256 rows
 constexpr int kAttnTargetWGs = 256;         // workgroups the bf16 planner splits the prefix for: one a compute unit
+// Bounded views: up to this many rows of a GQA group the kernel for few rows takes
+// them, in blocks of 16 or 32.
+constexpr int kViewFewRows = 32;
+constexpr int kViewFewTargetWGs = 512;  // two workgroups of four waves a compute unit
+constexpr int kViewFewMinTiles = 8;     // 32-key tiles that a split keeps: two a wave
 // float32 path: query rows per workgroup.  32 rows read each key half as often
 // as 16; 16 rows make twice as many workgroups, which pays where 32 leave
 // compute units idle (16/8 heads x 64 tokens, D = 128, 16 and 32 rows: 2048 keys,
@@ -242,14 +283,35 @@ constexpr int conf_tile_rows(int n_rows) { return n_rows <= kConfSmallMaxRows ? 
 constexpr int kConfF32MinIds = 128;
 constexpr int conf_f32_tile_rows(int n_rows) { return n_rows <= 32 ? 32 : 64; }
 
+// launch(p) over the work items of p in grids of at most kAttnMaxGrid workgroups
+// (heavy_first takes one grid; the host asks for it only where that holds them).
+template <class Launch>
+void for_each_view_launch(ViewParams p, Launch&& launch) {
+  const int n = p.n_items;
+  for (int i = 0; i < n; i += p.n_items) {
+    p.item0 = i;
+    p.n_items = n - i < kAttnMaxGrid ? n - i : kAttnMaxGrid;
+    p.per_xcd = (p.n_items + 7) / 8;
+    launch(p);
+  }
+}
+
 hipError_t launch_slot_attn_bf16(const AttnParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_slot_attn_f32(const AttnParams32& p, int head_dim, hipStream_t stream);
+hipError_t launch_slot_attn_merge(const AttnParams& p, int head_dim, hipStream_t stream);  // of the prefix splits
+// `codes`: the caches hold 4-bit codes
+hipError_t launch_slot_view_bf16(const ViewParams& p, int head_dim, bool codes, hipStream_t stream);
+hipError_t launch_slot_view_few(const ViewParams& p, int head_dim, bool codes, hipStream_t stream);  // blocks of 16 or 32 rows
+hipError_t launch_slot_view_f32(const ViewParams32& p, int head_dim, bool codes, hipStream_t stream);
 hipError_t launch_slot_conf_bf16(const ConfParams& p, hipStream_t stream);
 hipError_t launch_slot_conf_f32(const ConfParams& p, hipStream_t stream);
 hipError_t launch_slot_conf_merge(const ConfMergeParams& p, hipStream_t stream);
 hipError_t launch_select_slots(const SelectParams& p, hipStream_t stream);
 hipError_t launch_verify_accept(const AcceptParams& p, hipStream_t stream);
 hipError_t launch_kv_append(const AppendParams& p, hipStream_t stream);
+hipError_t launch_kv_quantize(const KvQ4Params& p, hipStream_t stream);
+hipError_t launch_kv_dequantize(const KvQ4Params& p, hipStream_t stream);
+hipError_t launch_kv_append_q4(const AppendQ4Params& p, hipStream_t stream);
 hipError_t launch_mdm_reveal(const RevealParams& p, hipStream_t stream);
 
 }  // namespace zarya

@@ -1,0 +1,444 @@
+// Slot attention over a bounded view of the prefix for few query rows (gfx950):
+// single tokens and short slots, where a block of 128 rows would be mostly
+// padding and the cache's bytes are what counts.
+//
+// One workgroup = 4 waves = 16 * NT query rows of one GQA group (token-major, as in
+// slot_attn.hip) and one share of the key tiles.  The waves share the rows and
+// split the keys: a wave takes every fourth tile of 32 keys, keeps its own online
+// softmax and meets the others in LDS at the end.  Nothing is staged: a lane reads
+// the codes (or elements) of its own keys straight into the registers that the
+// matrix instructions take them from, one tile ahead.
+//
+//  * S^T = K Q^T with v_mfma_f32_16x16x32_bf16: lane quarter q (16 lanes) of a key's
+//    row holds the elements [q * D/4, (q + 1) * D/4), which in 4 bits at D = 128
+//    are one 16-byte block with one scale.  Row m of product a is key
+//    8 * (m / 4) + m % 4 of the tile and of product b the key 4 further, so that
+//    quarter q of the scores holds the keys 8q .. 8q + 7 in order: the B operand
+//    of O^T += V^T P^T as it stands.
+//  * Of V a lane reads the D/16 elements [m * D/16, (m + 1) * D/16) of its quarter's
+//    eight keys: 4 bytes a key in 4 bits at D = 128.  Row m of output block i is
+//    element m * D/16 + i; pairs of keys are brought together with v_perm.
+//  * 4-bit codes are converted by the block-scaled conversions (exact in bf16).
+#include <algorithm>
+#include <type_traits>
+
+#include "attn_view.hpp"
+#include "common.hpp"
+#include "kernels.hpp"
+
+namespace zarya {
+
+namespace {
+
+constexpr int FKT = 32;     // keys per tile
+constexpr int FNW = 4;      // waves per workgroup
+constexpr float kRescaleLog2 = 8.f;  // growth of a row maximum (log2 units) that forces a rescale
+
+__device__ __forceinline__ f32x4 mfma16x16x32(const bf16x8& a, const bf16x8& b, const f32x4& c) {
+  return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
+}
+
+// max(x, x of lane ^ 16) through the VALU exchange of neighbouring rows of 16 lanes
+__device__ __forceinline__ float max_xor16(float x) {
+  const auto r = __builtin_amdgcn_permlane16_swap(__float_as_uint(x), __float_as_uint(x), false, false);
+  return __builtin_fmaxf(__uint_as_float(r[0]), __uint_as_float(r[1]));
+}
+
+}  // namespace
+
+// A tile's bytes on their way: 4-bit codes and scales, or elements in bf16.
+template <int D, bool Q4>
+struct FewRaw;
+
+template <int D>
+struct FewRaw<D, true> {
+  static constexpr int KW = D / 32;  // words of codes per K quarter row
+  uint32_t k[2][KW];
+  uint32_t ks[2];
+  uint32_t v[8];   // D/16 codes of each of eight keys
+  uint32_t vs[8];  // a key's scales, the lane's own in the low byte (D = 64: 16-bit pieces)
+};
+
+template <int D>
+struct FewRaw<D, false> {
+  uint4 k[2][D / 32];      // D/4 elements
+  uint4 v[8][D / 128 + (D < 128)];  // D/16 elements (D = 64: 8 bytes, in x and y)
+};
+
+template <int D, int NT, bool Q4>
+__global__ __launch_bounds__(FNW * 64) __attribute__((amdgpu_waves_per_eu(2))) void slot_view_few_kernel(ViewParams p) {
+  constexpr int RB = 16 * NT;
+  constexpr int NKS = D / 32;  // k-steps of the QK^T contraction
+  constexpr int NOB = D / 16;  // 16-wide blocks of the output = elements of a V row per lane
+  constexpr int OSTR = D + 4;  // row stride of the partial outputs in LDS
+  __shared__ __attribute__((aligned(16))) float part_o[FNW][RB][OSTR];
+  __shared__ float part_m[FNW][RB], part_l[FNW][RB];
+
+  int w = xcd_work_index(blockIdx.x, p.per_xcd, p.n_items);
+  if (w < 0) return;
+  w += p.item0;
+  const int rb = w % p.n_rb;
+  const int split = (w / p.n_rb) % p.n_split;
+  const int bg = w / (p.n_rb * p.n_split);
+  const int b = bg / p.Hkv;
+  const int Pb = p.prefix_lens ? min(max(p.prefix_lens[b], 0), p.P) : p.P;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, q4 = lane >> 4;
+  const int t0 = rb * RB / p.G, t1 = (min(p.R, rb * RB + RB) - 1) / p.G;
+
+  KeyTiles<FKT> tiles;
+  tiles.list(Pb, t0, p.cross ? 0 : t0 / p.L * p.L,
+             p.pass != 0 && !p.slot_pass ? t1 + 1 : min(p.T, (t1 / p.L + 1) * p.L), p.window, p.sinks);
+  // this workgroup's tiles, of which the wave takes every fourth: the prefix's
+  // first, the draft tokens' after them
+  const int per_split = (tiles.nt + p.n_split - 1) / p.n_split;
+  const int first = min(split * per_split, tiles.nt), end = min(tiles.nt, first + per_split);
+  const int pre_end = min(end, tiles.n_pre);
+
+  // the lane's rows: visible draft keys, and the first draft key inside the window
+  int vis_lo[NT], vis_hi[NT], win_lo[NT];
+  bf16x8 qf[NT][NKS];
+#pragma unroll
+  for (int r = 0; r < NT; ++r) {
+    const int row = min(rb * RB + 16 * r + n, p.R - 1);  // rows past the end follow the last one
+    const int t = row / p.G, s = t / p.L;
+    const int pass = p.slot_pass ? (int)p.slot_pass[b * p.S + s] : p.pass;
+    vis_hi[r] = pass == 0 ? (s + 1) * p.L : t + 1;
+    vis_lo[r] = p.cross ? 0 : s * p.L;
+    win_lo[r] = t - p.window + 1;
+    const uint16_t* qrow = p.q + ((size_t)bg * p.R + (size_t)(row % p.G) * p.T + t) * D + q4 * (D / 4);
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) qf[r][ks] = *reinterpret_cast<const bf16x8*>(qrow + 8 * ks);
+  }
+
+  f32x4 oacc[NT][NOB];
+  float m[NT], l[NT];
+#pragma unroll
+  for (int r = 0; r < NT; ++r) {
+    m[r] = kNegBig;
+    l[r] = 0.f;
+#pragma unroll
+    for (int ob = 0; ob < NOB; ++ob) oacc[r][ob] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+  const float c2 = p.scale_log2;
+  const int ka = 8 * (n >> 2) + (n & 3);  // the tile's key in row n of product a
+
+  // K and V of one tile -> registers.  Keys past the last one follow it (their
+  // scores are masked); whole tiles need no such care.
+  auto fetch = [&](auto& raw, bool pre, int key0) __attribute__((always_inline)) {
+    const int last = (pre ? Pb : p.T) - 1 - key0;
+    const bool whole = last >= FKT - 1;
+    auto at = [&](int k) { return whole ? k : min(k, last); };
+    if constexpr (std::is_same_v<std::decay_t<decltype(raw)>, FewRaw<D, true>>) {
+      const size_t base = (size_t)bg * p.C + key0;
+      const uint8_t* kc = reinterpret_cast<const uint8_t*>(p.k_cache) + base * (D / 2);
+      const uint8_t* vc = reinterpret_cast<const uint8_t*>(p.v_cache) + base * (D / 2);
+      const uint8_t* kscale = p.k_scale + base * (D / 32);
+      const uint8_t* vscale = p.v_scale + base * (D / 32);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const uint32_t k = at(ka + 4 * t);
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(kc + k * (D / 2) + q4 * (D / 8));
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) raw.k[t][e] = src[e];
+        raw.ks[t] = kscale[k * (D / 32) + q4 * (D / 4) / 32];
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint32_t k = at(8 * q4 + j);
+        if constexpr (D == 128) {
+          raw.v[j] = *reinterpret_cast<const uint32_t*>(vc + k * (D / 2) + n * 4);
+        } else {
+          raw.v[j] = *reinterpret_cast<const uint16_t*>(vc + k * (D / 2) + n * 2);
+        }
+        raw.vs[j] = vscale[k * (D / 32) + n * (D / 16) / 32];
+      }
+    } else {
+      const size_t base = pre ? (size_t)bg * p.C + key0 : (size_t)bg * p.T + key0;
+      const uint16_t* kc = (pre ? p.k_cache : p.k_slot) + base * D;
+      const uint16_t* vc = (pre ? p.v_cache : p.v_slot) + base * D;
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        const uint4* src = reinterpret_cast<const uint4*>(kc + (uint32_t)at(ka + 4 * t) * D + q4 * (D / 4));
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) raw.k[t][e] = src[e];
+      }
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const uint16_t* src = vc + (uint32_t)at(8 * q4 + j) * D + n * (D / 16);
+        if constexpr (D == 128) {
+          raw.v[j][0] = *reinterpret_cast<const uint4*>(src);
+        } else {
+          const uint2 v = *reinterpret_cast<const uint2*>(src);
+          raw.v[j][0] = make_uint4(v.x, v.y, 0, 0);
+        }
+      }
+    }
+  };
+
+  // scores, online softmax and value products of one tile
+  auto compute = [&](const auto& raw, bool pre, int key0) __attribute__((always_inline)) {
+    constexpr bool Codes = std::is_same_v<std::decay_t<decltype(raw)>, FewRaw<D, true>>;
+    f32x4 s[NT][2];
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      bf16x8 kf[NKS];
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) {
+        if constexpr (Codes) {
+          kf[ks] = q4_bf16x8(raw.k[t][ks], q4_scale(raw.ks[t]));
+        } else {
+          kf[ks] = __builtin_bit_cast(bf16x8, raw.k[t][ks]);
+        }
+      }
+#pragma unroll
+      for (int r = 0; r < NT; ++r) {
+        s[r][t] = f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) s[r][t] = mfma16x16x32(kf[ks], qf[r][ks], s[r][t]);
+      }
+    }
+    const int off = pre ? Pb : 0;  // places of the tile's keys less their indices, as seen from the tokens
+    const int sink_hi = p.sinks - (pre ? 0 : Pb);
+    const bool shown = pre ? key0 + FKT <= Pb
+                           : key0 >= (p.cross ? 0 : t1 / p.L * p.L) && key0 + FKT <= t0 + 1;
+    const bool masked = !(shown && (key0 + FKT <= sink_hi || key0 > off + t1 - p.window));
+    bf16x8 pb[NT];
+#pragma unroll
+    for (int r = 0; r < NT; ++r) {
+      if (masked) {
+        auto below = [&](int x) { return x <= key0 ? 0u : x - key0 >= FKT ? ~0u : (1u << (x - key0)) - 1; };
+        const uint32_t range = pre ? below(Pb) : below(vis_hi[r]) & ~below(vis_lo[r]);
+        const uint32_t seen = (range & (below(sink_hi) | ~below(win_lo[r] + off))) >> (8 * q4);
+#pragma unroll
+        for (int t = 0; t < 2; ++t)
+#pragma unroll
+          for (int v = 0; v < 4; ++v)
+            if (!(seen >> (4 * t + v) & 1)) s[r][t][v] = -INFINITY;
+      }
+      float mt = max3f(max3f(s[r][0][0], s[r][0][1], s[r][0][2]), s[r][0][3], s[r][1][0]);
+      mt = max3f(max3f(mt, s[r][1][1], s[r][1][2]), s[r][1][3], s[r][1][3]);
+      mt = max_xor32(max_xor16(mt));
+      const float m_new = fmaxf(m[r], mt);
+      // as in attn_bf16_body: sums are rescaled only once a maximum has grown by 2^8
+      if (__any((m_new - m[r]) * c2 > kRescaleLog2)) {
+        const float alpha = fast_exp2((m[r] - m_new) * c2);
+        l[r] *= alpha;
+#pragma unroll
+        for (int ob = 0; ob < NOB; ++ob)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) oacc[r][ob][v] *= alpha;
+        m[r] = m_new;
+      }
+      const float mc = m[r] * c2;
+      uint32_t pk[4];
+#pragma unroll
+      for (int j = 0; j < 8; j += 2) {
+        const float e0 = fast_exp2(fmaf(s[r][j >> 2][j & 3], c2, -mc));
+        const float e1 = fast_exp2(fmaf(s[r][j >> 2][(j & 3) + 1], c2, -mc));
+        l[r] += e0 + e1;
+        pk[j >> 1] = pack_bf16x2_hw(e0, e1);
+      }
+      pb[r] = __builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3]));
+    }
+    // element pair (2e, 2e + 1) of the lane's part of key j's V row, as packed bf16
+    float vsc[8];
+    if constexpr (Codes) {
+#pragma unroll
+      for (int j = 0; j < 8; ++j) vsc[j] = q4_scale(raw.vs[j]);
+    }
+#pragma unroll
+    for (int e = 0; e < NOB / 2; ++e) {
+      uint32_t w[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        if constexpr (Codes) {
+          bf16x2_t x;
+          if (e == 0) x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(raw.v[j], vsc[j], 0);
+          if (e == 1) x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(raw.v[j], vsc[j], 1);
+          if (e == 2) x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(raw.v[j], vsc[j], 2);
+          if (e == 3) x = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(raw.v[j], vsc[j], 3);
+          w[j] = __builtin_bit_cast(uint32_t, x);
+        } else {
+          w[j] = e == 0 ? raw.v[j][0].x : e == 1 ? raw.v[j][0].y : e == 2 ? raw.v[j][0].z : raw.v[j][0].w;
+        }
+      }
+      uint32_t lo[4], hi[4];  // the keys in pairs: elements 2e, and 2e + 1
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        lo[j] = __builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], 0x05040100);
+        hi[j] = __builtin_amdgcn_perm(w[2 * j + 1], w[2 * j], 0x07060302);
+      }
+      const bf16x8 a0 = __builtin_bit_cast(bf16x8, make_uint4(lo[0], lo[1], lo[2], lo[3]));
+      const bf16x8 a1 = __builtin_bit_cast(bf16x8, make_uint4(hi[0], hi[1], hi[2], hi[3]));
+#pragma unroll
+      for (int r = 0; r < NT; ++r) {
+        oacc[r][2 * e] = mfma16x16x32(a0, pb[r], oacc[r][2 * e]);
+        oacc[r][2 * e + 1] = mfma16x16x32(a1, pb[r], oacc[r][2 * e + 1]);
+      }
+    }
+  };
+
+  if constexpr (!Q4 && D == 128 && NT == 2) {  // no registers left to read ahead
+    for (int i = first + wave; i < pre_end; i += FNW) {
+      FewRaw<D, false> raw;
+      fetch(raw, true, tiles.key0(i));
+      compute(raw, true, tiles.key0(i));
+    }
+  } else {
+    FewRaw<D, Q4> raw[2];
+    int i = first + wave;
+    if (i < pre_end) fetch(raw[0], true, tiles.key0(i));
+    while (i < pre_end) {
+      if (i + FNW < pre_end) fetch(raw[1], true, tiles.key0(i + FNW));
+      compute(raw[0], true, tiles.key0(i));
+      i += FNW;
+      if (i >= pre_end) break;
+      if (i + FNW < pre_end) fetch(raw[0], true, tiles.key0(i + FNW));
+      compute(raw[1], true, tiles.key0(i));
+      i += FNW;
+    }
+  }
+  // the draft tokens' tiles go round from the wave after the prefix's last one
+  for (int i = max(first, tiles.n_pre) + ((wave + FNW - (max(first, tiles.n_pre) - first) % FNW) & (FNW - 1)); i < end;
+       i += FNW) {
+    FewRaw<D, false> raw;
+    fetch(raw, false, tiles.key0(i));
+    compute(raw, false, tiles.key0(i));
+  }
+
+  // ---- values that are not finite: as in attn_bf16_body, the wave's sums once
+  // more, key by key over the visible ones
+  {
+    float z = 0.f;
+#pragma unroll
+    for (int r = 0; r < NT; ++r)
+#pragma unroll
+      for (int ob = 0; ob < NOB; ++ob)
+#pragma unroll
+        for (int v = 0; v < 4; ++v) z = fmaf(oacc[r][ob][v], 0.f, z);
+    if (__any(z != 0.f)) {
+#pragma unroll
+      for (int r = 0; r < NT; ++r)
+#pragma unroll
+        for (int ob = 0; ob < NOB; ++ob) oacc[r][ob] = f32x4{0.f, 0.f, 0.f, 0.f};
+      auto row8 = [&](bool pre, int which, int key, int d) __attribute__((always_inline)) {
+        if (Q4 && pre) {
+          const size_t at = (size_t)bg * p.C + key;
+          const uint8_t* cp = reinterpret_cast<const uint8_t*>(which ? p.v_cache : p.k_cache) + at * (D / 2) + d / 2;
+          return q4_bf16x8(*reinterpret_cast<const uint32_t*>(cp),
+                           q4_scale((which ? p.v_scale : p.k_scale)[at * (D / 32) + d / 32]));
+        }
+        const uint16_t* base = pre ? (which ? p.v_cache : p.k_cache) : which ? p.v_slot : p.k_slot;
+        return *reinterpret_cast<const bf16x8*>(base + ((size_t)bg * (pre ? p.C : p.T) + key) * D + d);
+      };
+#pragma unroll 1
+      for (int i = first + wave; i < end; i += FNW) {
+        const bool pre = i < tiles.n_pre;
+        const int key0 = tiles.key0(i), kend = min(key0 + FKT, pre ? Pb : p.T), off = pre ? Pb : 0;
+#pragma unroll 1
+        for (int key = key0; key < kend; ++key) {
+#pragma unroll
+          for (int r = 0; r < NT; ++r) {
+            const bool ok = (pre || (key >= vis_lo[r] && key < vis_hi[r])) &&
+                            (key < p.sinks - (pre ? 0 : Pb) || key >= win_lo[r] + off);
+            if (!__any(ok)) continue;
+            float sc = 0.f;
+#pragma unroll
+            for (int ks = 0; ks < NKS; ++ks) {
+              const bf16x8 kv = row8(pre, 0, key, q4 * (D / 4) + 8 * ks);
+#pragma unroll
+              for (int e = 0; e < 8; ++e) sc = fmaf((float)qf[r][ks][e], (float)kv[e], sc);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+            sc += __shfl_xor(sc, 16);
+            sc = sum_xor32(sc);
+            const float pr = (float)(__bf16)fast_exp2(fmaf(sc, c2, -(m[r] * c2)));
+            // oacc[ob][v] is element (4 * q4 + v) * D/16 + ob
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const bf16x8 vv = row8(pre, 1, key, ((4 * q4 + v) * NOB) & ~7);
+#pragma unroll
+              for (int ob = 0; ob < NOB; ++ob) {
+                const float x = (float)vv[(v * NOB + ob) & 7];
+                oacc[r][ob][v] = ok ? fmaf(pr, x, oacc[r][ob][v]) : oacc[r][ob][v];
+              }
+              __builtin_amdgcn_sched_barrier(0);  // one piece at a time: few registers
+            }
+          }
+        }
+      }
+    }
+  }
+
+  // ---- merge of the waves' partials, in wave order
+#pragma unroll
+  for (int r = 0; r < NT; ++r) {
+    l[r] += __shfl_xor(l[r], 16);
+    l[r] = sum_xor32(l[r]);
+    const int lr = 16 * r + n;
+    if (q4 == 0) {
+      part_m[wave][lr] = m[r];
+      part_l[wave][lr] = l[r];
+    }
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+#pragma unroll
+      for (int ob = 0; ob < NOB; ob += 4)
+        *reinterpret_cast<f32x4*>(&part_o[wave][lr][(4 * q4 + v) * NOB + ob]) =
+            f32x4{oacc[r][ob][v], oacc[r][ob + 1][v], oacc[r][ob + 2][v], oacc[r][ob + 3][v]};
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < RB * (D / 4); x += FNW * 64) {
+    const int lr = x / (D / 4), c = 4 * (x % (D / 4));
+    const int row = rb * RB + lr;
+    if (row >= p.R) break;
+    float mx = part_m[0][lr];
+#pragma unroll
+    for (int i = 1; i < FNW; ++i) mx = fmaxf(mx, part_m[i][lr]);
+    float lt = 0.f;
+    f32x4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < FNW; ++i) {
+      const float sc = fast_exp2((part_m[i][lr] - mx) * c2);  // 0 for a wave without a visible key
+      lt += sc * part_l[i][lr];
+      o += sc * *reinterpret_cast<const f32x4*>(&part_o[i][lr][c]);
+    }
+    const float inv = lt > 0.f ? 1.f / lt : 0.f;
+    const float lse2 = mx * c2 + __log2f(lt);  // log2 units
+    const size_t grow = (size_t)bg * p.R + (size_t)(row % p.G) * p.T + row / p.G;
+    if (p.n_split == 1) {
+      *reinterpret_cast<uint2*>(p.out + grow * D + c) =
+          make_uint2(pack_bf16x2_hw(o[0] * inv, o[1] * inv), pack_bf16x2_hw(o[2] * inv, o[3] * inv));
+      if (p.lse && c == 0) p.lse[grow] = lse2 * kLn2;
+    } else {
+      const size_t prow = (size_t)split * p.rows_total + grow;
+      *reinterpret_cast<f32x4*>(p.part_o + prow * D + c) = f32x4{o[0] * inv, o[1] * inv, o[2] * inv, o[3] * inv};
+      if (c == 0) p.part_lse[prow] = lt > 0.f ? lse2 : -INFINITY;
+    }
+  }
+}
+
+template <int D, bool Q4>
+static void launch_few_as(const ViewParams& all, hipStream_t stream) {
+  for_each_view_launch(all, [&](const ViewParams& p) {
+    if (p.rows_per_block == 16) {
+      slot_view_few_kernel<D, 1, Q4><<<dim3(8 * p.per_xcd), dim3(FNW * 64), 0, stream>>>(p);
+    } else {
+      slot_view_few_kernel<D, 2, Q4><<<dim3(8 * p.per_xcd), dim3(FNW * 64), 0, stream>>>(p);
+    }
+  });
+}
+
+hipError_t launch_slot_view_few(const ViewParams& p, int head_dim, bool codes, hipStream_t stream) {
+  if (codes) {
+    head_dim == 128 ? launch_few_as<128, true>(p, stream) : launch_few_as<64, true>(p, stream);
+  } else {
+    head_dim == 128 ? launch_few_as<128, false>(p, stream) : launch_few_as<64, false>(p, stream);
+  }
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || p.n_split == 1 ? e : launch_slot_attn_merge(p, head_dim, stream);
+}
+
+}  // namespace zarya

@@ -17,6 +17,7 @@
 
 #include "common.hpp"
 #include "kernels.hpp"
+#include "kv_q4.hpp"
 
 namespace zarya {
 
@@ -94,7 +95,9 @@ __global__ __launch_bounds__(MAXT) void verify_accept_kernel(AcceptParams p) {
 // and move the row's prefix length.  `lg`: log2 of the lanes per slot.
 // B = 16, 8 heads, 4 of 8 slots with 7 of 8 tokens: 9.4 -> 7.2 us (256 threads,
 // a serial scan over the slots and a thread per slot reading its flags).
-__global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendParams p, int lg) {
+// Q4: into the 4-bit cache, eight elements a lane.
+template <bool Q4, class Params>
+__device__ __forceinline__ void kv_append_body(const Params& p, int lg) {
   __shared__ int slot_of[1024];   // order position -> slot id (or -1)
   __shared__ int count_of[1024];  // order position -> accepted tokens of that slot
   __shared__ int start_of[1024];  // order position -> first index in `tokens`
@@ -163,6 +166,23 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendParams p, int
   __syncthreads();
   each_accepted([&](int i, int token, int rank) { tokens[start_of[i] + rank] = token; }, [](int, int) {});
   __syncthreads();
+  if constexpr (Q4) {
+    const int lp = __builtin_ctz(p.D / 8);
+    const int total = (p.Hkv * n) << lp;  // a multiple of 4: the lanes of a block run together
+    for (int e = tid; e < total; e += kThreads) {
+      const int x = e >> lp, c = e & ((1 << lp) - 1);
+      const int g = x / n, i = x - g * n;
+      const size_t src = (((size_t)b * p.Hkv + g) * T + tokens[i]) * p.D + 8 * c;
+      const size_t dst = ((size_t)b * p.Hkv + g) * p.C + p0 + i;
+      float k[8], v[8];
+      load_f32x8(p.k_slot, src, p.bf16, k);
+      load_f32x8(p.v_slot, src, p.bf16, v);
+      store_q4(p.cache.k_codes, p.cache.k_scales, dst, p.D, c, k);
+      store_q4(p.cache.v_codes, p.cache.v_scales, dst, p.D, c, v);
+    }
+    if (tid == 0) p.prefix_lens[b] = p0 + n;
+    return;
+  }
   const int lp = __builtin_ctz(p.row_bytes / 16);  // 16-byte pieces of a row: 8, 16 or 32
   // one flat loop over (head, token, 16-byte piece): every thread's loads are
   // independent of its stores (the slot K/V and the cache never overlap), so
@@ -186,6 +206,14 @@ __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendParams p, int
   if (tid == 0) p.prefix_lens[b] = p0 + n;
 }
 
+__global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendParams p, int lg) {
+  kv_append_body<false, AppendParams>(p, lg);
+}
+
+__global__ __launch_bounds__(kThreads) void kv_append_q4_kernel(AppendQ4Params p, int lg) {
+  kv_append_body<true, AppendQ4Params>(p, lg);
+}
+
 hipError_t launch_verify_accept(const AcceptParams& p, hipStream_t stream) {
   // 1024 threads a row, of which a unit holds two, where the rows alone do not
   // fill the units; with many rows up to 256 and no more than tokens (4096 rows: 64
@@ -200,10 +228,19 @@ hipError_t launch_verify_accept(const AcceptParams& p, hipStream_t stream) {
   return hipGetLastError();
 }
 
-hipError_t launch_kv_append(const AppendParams& p, hipStream_t stream) {
+static int lanes_log2(int slot_len) {
   int lg = 0;  // a lane per token of a slot, up to a wave
-  while (lg < 6 && (1 << lg) < p.L) ++lg;
-  kv_append_kernel<<<dim3(p.B), dim3(kThreads), 0, stream>>>(p, lg);
+  while (lg < 6 && (1 << lg) < slot_len) ++lg;
+  return lg;
+}
+
+hipError_t launch_kv_append(const AppendParams& p, hipStream_t stream) {
+  kv_append_kernel<<<dim3(p.B), dim3(kThreads), 0, stream>>>(p, lanes_log2(p.L));
+  return hipGetLastError();
+}
+
+hipError_t launch_kv_append_q4(const AppendQ4Params& p, hipStream_t stream) {
+  kv_append_q4_kernel<<<dim3(p.B), dim3(kThreads), 0, stream>>>(p, lanes_log2(p.L));
   return hipGetLastError();
 }
 
