@@ -13,7 +13,7 @@ namespace {
 
 struct ViewPlan {
   int T, G, R;
-  int rows_per_block, n_rb, n_split;
+  int rows_per_block, n_rb, n_split, key_groups;
   int64_t rows_total, items;
   size_t ws_o, ws_bytes;  // bytes of the partial outputs; of the whole workspace
 };
@@ -34,50 +34,76 @@ zarya_status check_view(const zarya_slot_attn_desc* d, const zarya_attn_window* 
   return ZARYA_OK;
 }
 
-ViewPlan plan_view(const zarya_slot_attn_desc* d, const zarya_attn_window* w) {
+// Splits of blocks of 128 or 256 rows.  `base` blocks with `tiles` key tiles each, of
+// which a workgroup takes `tile_ns` a tile, are split no further than to a workgroup
+// a unit; a split costs the merge's launch, and its partials' way to memory and back.
+int best_splits(int64_t base, int64_t tiles, int64_t tile_ns, int64_t partial_bytes, int64_t* cost) {
+  const int64_t most = std::max<int64_t>(1, std::min<int64_t>({64, tiles, kAttnTargetWGs / base}));
+  int best = 1;
+  *cost = tiles * tile_ns * ((base + kAttnTargetWGs - 1) / kAttnTargetWGs);
+  for (int ns = 2; ns <= most; ++ns) {
+    const int64_t c = (tiles * tile_ns + ns - 1) / ns + kViewMergeNs + ns * partial_bytes / kViewPartialBytesPerNs;
+    if (c < *cost) {
+      *cost = c;
+      best = ns;
+    }
+  }
+  return best;
+}
+
+ViewPlan plan_view(const zarya_slot_attn_desc* d, const zarya_attn_window* w, bool codes) {
   ViewPlan pl{};
   pl.T = d->n_slots * d->slot_len;
   pl.G = d->n_q_heads / d->n_kv_heads;
   pl.R = pl.G * pl.T;
   pl.rows_total = (int64_t)d->batch * d->n_q_heads * pl.T;
-  pl.n_split = 1;
+  pl.n_split = pl.key_groups = 1;
   if (d->dtype == ZARYA_DTYPE_F32) return pl;
   const int64_t groups = (int64_t)d->batch * d->n_kv_heads;
   // prefix keys that a row block sees at most, its own tokens' shift of the window aside
   const int64_t seen = std::min<int64_t>(d->prefix_len, (int64_t)window_of(w) + sinks_of(w));
-  int64_t want;    // splits that fill the units
-  int64_t tiles;   // key tiles, and how many of them a split has to keep
-  if (pl.R <= kViewFewRows) {
+  int64_t ns, most;  // splits taken, and the most that a shorter prefix could take
+  if (pl.R <= (codes ? kViewFewRowsCodes : kViewFewRows)) {
     pl.rows_per_block = pl.R <= 16 ? 16 : 32;
     pl.n_rb = (pl.R + pl.rows_per_block - 1) / pl.rows_per_block;
-    want = kViewFewTargetWGs / (groups * pl.n_rb);
-    tiles = (seen + 31) / 32 / kViewFewMinTiles;
+    const int64_t base = groups * pl.n_rb, tiles = (seen + 31) / 32;
+    ns = std::max(std::min<int64_t>({kViewFewTargetWGs / base, tiles / kViewFewMinTiles, 32}),
+                  std::min<int64_t>(kViewFewBalanceWGs / base, tiles / kViewFewBalanceTiles));
+    ns = most = std::max<int64_t>(1, ns);
   } else {
     const int n_narrow = (pl.R + kAttnRowsPerBlock - 1) / kAttnRowsPerBlock;
     const int n_wide = (pl.R + kAttnWideRowsPerBlock - 1) / kAttnWideRowsPerBlock;
-    const bool wide = 2 * n_wide <= n_narrow && seen >= pl.T;
+    const int64_t tiles = (seen + std::min(pl.T, d->cross_slot ? pl.T : 2 * d->slot_len)) / kAttnKeysPerTile + 1;
+    const int64_t partial = pl.rows_total * d->head_dim * 4;
+    const ViewTileNs t = view_tile_ns(codes, d->head_dim);
+    int64_t cost_narrow, cost_wide;
+    const bool pairs = groups * n_narrow > kAttnTargetWGs;  // two workgroups a unit instead of two key groups in one
+    const int ns_narrow = best_splits(pairs ? (groups * n_narrow + 1) / 2 : groups * n_narrow, tiles,
+                                      pairs ? t.narrow_pair : t.narrow, partial, &cost_narrow);
+    const int ns_wide = best_splits(groups * n_wide, tiles, t.wide, partial, &cost_wide);
+    const bool whole = 2 * n_wide <= n_narrow;  // 256-row blocks add no padding waves
+    const bool wide = whole && seen >= pl.T && cost_wide < cost_narrow;
     pl.rows_per_block = wide ? kAttnWideRowsPerBlock : kAttnRowsPerBlock;
     pl.n_rb = wide ? n_wide : n_narrow;
-    want = kAttnTargetWGs / (groups * pl.n_rb);
-    tiles = (seen + kAttnKeysPerTile - 1) / kAttnKeysPerTile / 4;
+    ns = wide ? ns_wide : ns_narrow;
+    most = whole ? std::max(ns_wide, ns_narrow) : ns_narrow;
   }
-  const int64_t ns = d->prefix_splits > 0 ? std::min<int64_t>(d->prefix_splits, std::max<int64_t>(1, (seen + 31) / 32))
-                                          : std::min(want, tiles);
-  pl.n_split = (int)std::max<int64_t>(1, std::min<int64_t>(ns, 64));
-  pl.items = groups * pl.n_rb * pl.n_split;
-  if (pl.n_split > 1) {
-    pl.ws_o = align256((size_t)pl.n_split * pl.rows_total * d->head_dim * 4);
-    pl.ws_bytes = pl.ws_o + align256((size_t)pl.n_split * pl.rows_total * 4);
+  if (d->prefix_splits > 0) ns = most = std::min<int64_t>(d->prefix_splits, std::max<int64_t>(1, (seen + 31) / 32));
+  pl.n_split = (int)ns;
+  pl.items = groups * pl.n_rb * ns;
+  if (pl.rows_per_block == kAttnRowsPerBlock && pl.items <= kAttnTargetWGs) pl.key_groups = 2;
+  if (most > 1) {
+    pl.ws_o = align256((size_t)ns * pl.rows_total * d->head_dim * 4);
+    pl.ws_bytes = align256((size_t)most * pl.rows_total * d->head_dim * 4) + align256((size_t)most * pl.rows_total * 4);
   }
   return pl;
 }
 
-zarya_status view_workspace_size(const zarya_slot_attn_desc* d, const zarya_attn_window* w, bool window_required,
-                                 size_t* bytes) {
+zarya_status view_workspace_size(const zarya_slot_attn_desc* d, const zarya_attn_window* w, bool codes, size_t* bytes) {
   if (!bytes) return fail(ZARYA_ERR_INVALID_ARGUMENT, "bytes is NULL");
-  const zarya_status st = check_view(d, w, window_required);
+  const zarya_status st = check_view(d, w, !codes);
   if (st != ZARYA_OK) return st;
-  *bytes = plan_view(d, w).ws_bytes;
+  *bytes = plan_view(d, w, codes).ws_bytes;
   return ZARYA_OK;
 }
 
@@ -127,7 +153,7 @@ zarya_status run_view(const zarya_slot_attn_desc* d, const zarya_attn_window* w,
     return fail(ZARYA_ERR_INVALID_ARGUMENT, "the cache arrays are required when prefix_len > 0");
   if (!aligned16({q, k_cache, v_cache, k_slot, v_slot, out, workspace}))
     return fail(ZARYA_ERR_INVALID_ARGUMENT, "q, the caches, the slot K/V, out and the workspace must be 16-byte aligned");
-  const ViewPlan pl = plan_view(d, w);
+  const ViewPlan pl = plan_view(d, w, codes);
   if (workspace_bytes < pl.ws_bytes)
     return fail(ZARYA_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes is below the %zu required", workspace_bytes,
                 pl.ws_bytes);
@@ -156,6 +182,7 @@ zarya_status run_view(const zarya_slot_attn_desc* d, const zarya_attn_window* w,
   p.n_items = (int)pl.items;
   p.per_xcd = (p.n_items + 7) / 8;
   p.rows_per_block = pl.rows_per_block;
+  p.key_groups = pl.key_groups;
   // as in zarya_slot_attn: under a causal order the row blocks with the most keys first
   const bool few = pl.rows_per_block < kAttnRowsPerBlock;
   const int64_t n_bg = (int64_t)d->batch * d->n_kv_heads;
@@ -213,7 +240,7 @@ extern "C" {
 
 zarya_status zarya_slot_attn_window_workspace_size(const zarya_slot_attn_desc* desc, const zarya_attn_window* window,
                                                    size_t* bytes) {
-  return view_workspace_size(desc, window, true, bytes);
+  return view_workspace_size(desc, window, /*codes=*/false, bytes);
 }
 
 zarya_status zarya_slot_attn_window(const zarya_slot_attn_desc* desc, const zarya_attn_window* window, const void* q,
@@ -228,7 +255,7 @@ zarya_status zarya_slot_attn_window(const zarya_slot_attn_desc* desc, const zary
 
 zarya_status zarya_slot_attn_q4_workspace_size(const zarya_slot_attn_desc* desc, const zarya_attn_window* window,
                                                size_t* bytes) {
-  return view_workspace_size(desc, window, false, bytes);
+  return view_workspace_size(desc, window, /*codes=*/true, bytes);
 }
 
 zarya_status zarya_slot_attn_q4(const zarya_slot_attn_desc* desc, const zarya_attn_window* window, const void* q,

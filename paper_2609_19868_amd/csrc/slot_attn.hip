@@ -81,7 +81,7 @@ __host__ __device__ constexpr int swz(int kr) {
 //
 // VIEW: 0 the whole prefix, 1 a window of it, 2 a cache of 4-bit codes (with or
 // without a window); see slot_view_bf16_kernel below.
-template <int D, int NWAVE, int VIEW, class Params>
+template <int D, int NWAVE, int VIEW, int GRP, class Params>
 __device__ __forceinline__ void attn_bf16_body(const Params& p) {
   constexpr int RB = NWAVE * 32;        // query rows per workgroup
   constexpr int ROWB = D * 2;           // bytes per key row
@@ -92,7 +92,7 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
   constexpr int NDB = D / 32;           // 32-wide blocks of the head dim
   constexpr int NKS = D / 16;           // k-steps of the QK^T contraction
   static_assert(CPW * NWAVE * 1024 == TILEB, "tile must split into 1 KB chunks per wave");
-  __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][TILEB];
+  __shared__ __attribute__((aligned(16))) uint8_t lds_all[GRP][2][2][TILEB];
 
   int rb, split, bg;  // row block, prefix split, b * Hkv + g
   if (p.heavy_first) {
@@ -119,7 +119,12 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
 
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = tid >> 6;
-  const int wave_u = __builtin_amdgcn_readfirstlane(wave);
+  const int wave_all = __builtin_amdgcn_readfirstlane(wave);
+  // GRP > 1: groups of NWAVE waves hold the same rows and take a share of the
+  // tiles each, with LDS buffers of their own
+  const int grp = GRP > 1 ? wave_all / NWAVE : 0;
+  const int wave_u = GRP > 1 ? wave_all % NWAVE : wave_all;
+  auto& lds = lds_all[grp];
   const int n = lane & 31, hh = lane >> 5;
 
   // ---- this lane's query row and its visible range [vis_lo, vis_hi) of
@@ -127,7 +132,7 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
   // h), so a block's rows cover a contiguous token range of every head of
   // the group and share one visible key range; mrow is the row's place in
   // the head-major [G, T] layout of q and out.
-  const int row = rb * RB + wave * 32 + n;
+  const int row = rb * RB + (GRP > 1 ? wave_u : wave) * 32 + n;
   const bool row_ok = row < p.R;
   const int mrow = (row % p.G) * p.T + row / p.G;
   int vis_lo = 0, vis_hi = 0;
@@ -162,6 +167,7 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
   // first + i; tokens tw0..tw1 are this wave's
   KeyTiles<KT> tiles;
   int first = 0, tw0 = 0, tw1 = 0;
+  int steps = 0;  // VIEW: tiles of the group that has the most
   if constexpr (VIEW != 0) {
     const int t0 = rb * RB / p.G, t1 = (min(p.R, rb * RB + RB) - 1) / p.G;
     tiles.list(Pb, t0, p.cross ? 0 : t0 / p.L * p.L,
@@ -169,6 +175,14 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
     const int per_split = (tiles.nt + p.n_split - 1) / p.n_split;
     first = min(split * per_split, tiles.nt);
     nt = min(per_split, tiles.nt - first);
+    if constexpr (GRP > 1) {
+      steps = (nt + GRP - 1) / GRP;
+      const int skip = min(grp * steps, nt);
+      first += skip;
+      nt = min(steps, nt - skip);
+    } else {
+      steps = nt;
+    }
     tw0 = (rb * RB + wave_u * 32) / p.G;
     tw1 = (min(p.R, rb * RB + wave_u * 32 + 32) - 1) / p.G;
   }
@@ -177,14 +191,18 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
   // ---- Q fragments (B operand of S^T = K Q^T), kept in registers; loaded
   // and waited for before the direct-load pipeline starts so that the
   // pipeline's counted waits see only its own loads
+  // (VIEW: after the first tile's loads, so that the two come together)
   bf16x8 qf[NKS];
-  {
+  auto load_q = [&]() __attribute__((always_inline)) {
     const uint4* qrow = reinterpret_cast<const uint4*>(p.q + ((size_t)bg * p.R + (row_ok ? mrow : 0)) * D);
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks) {
       uint4 v = row_ok ? qrow[2 * ks + hh] : make_uint4(0, 0, 0, 0);
       qf[ks] = __builtin_bit_cast(bf16x8, v);
     }
+  };
+  if constexpr (VIEW == 0) {
+    load_q();
 #pragma unroll
     for (int ks = 0; ks < NKS; ++ks) lds_tie(qf[ks]);
     wait_vmcnt<0>();
@@ -504,7 +522,7 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
     } else {
       if (i + 1 < nt) issue(i + 1, decltype(buf)::value ^ 1);
     }
-    if (!live) return;
+    if (!live || (GRP > 1 && i >= nt)) return;
     qk(buf);
     pv_read(buf, std::integral_constant<int, 0>{});  // in flight during the softmax
     softmax(i);
@@ -512,13 +530,20 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
   };
   if constexpr (VIEW == 2) {
     if (nt > 0 && is_pre(0)) fetch_q4(0);
+    load_q();
     advance(0, 0);
   } else {
     if (nt > 0) issue(0, 0);
+    if constexpr (VIEW != 0) load_q();
   }
-  for (int i = 0; i < nt; i += 2) {
+  if constexpr (VIEW != 0) {  // waited for here: in the loop it would be with every tile's loads
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) lds_tie(qf[ks]);
+  }
+  const int n_steps = GRP > 1 ? steps : nt;
+  for (int i = 0; i < n_steps; i += 2) {
     step(i, std::integral_constant<int, 0>{});
-    if (i + 1 < nt) step(i + 1, std::integral_constant<int, 1>{});
+    if (i + 1 < n_steps) step(i + 1, std::integral_constant<int, 1>{});
   }
 
   if constexpr (VIEW != 0) {
@@ -583,6 +608,31 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
     }
   }
 
+  if constexpr (GRP > 1) {
+    // the second group's sums to the first, lane by lane through the tile buffers
+    static_assert(GRP == 2 && NWAVE * (NDB * 16 + 2) * 64 * 4 <= (int)sizeof lds_all, "room for a group's sums");
+    float* x = reinterpret_cast<float*>(&lds_all[0][0][0][0]) + wave_u * (NDB * 16 + 2) * 64 + lane;
+    __syncthreads();
+    if (grp == 1) {
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) x[(db * 16 + v) * 64] = oacc[db][v];
+      x[NDB * 16 * 64] = m_run;
+      x[(NDB * 16 + 1) * 64] = l_run;
+    }
+    __syncthreads();
+    if (grp == 1) return;
+    const float m1 = x[NDB * 16 * 64], m_new = fmaxf(m_run, m1);
+    const float a0 = fast_exp2((m_run - m_new) * c2), a1 = fast_exp2((m1 - m_new) * c2);
+    l_run = l_run * a0 + x[(NDB * 16 + 1) * 64] * a1;
+    m_run = m_new;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) oacc[db][v] = oacc[db][v] * a0 + x[(db * 16 + v) * 64] * a1;
+  }
+
   // ---- finalize: combine the two lane halves' partial sums
   const float l_tot = sum_xor32(l_run);
   if (!row_ok) return;
@@ -592,7 +642,7 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
     // the same, instead of kept in a register through the loop
     int te = tid;
     asm volatile("" : "+v"(te));
-    const int row_e = rb * RB + (te >> 6) * 32 + (te & 31);
+    const int row_e = rb * RB + (GRP > 1 ? (te >> 6) % NWAVE : te >> 6) * 32 + (te & 31);
     orow_in = (row_e % p.G) * p.T + row_e / p.G;
   }
   const size_t grow = (size_t)bg * p.R + orow_in;  // row of the [B*Hq*T] output
@@ -629,13 +679,14 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
 template <int D, int NWAVE>
 __global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : ZARYA_ATTN_WPE))) void slot_attn_bf16_kernel(
     AttnParams p) {
-  attn_bf16_body<D, NWAVE, 0, AttnParams>(p);
+  attn_bf16_body<D, NWAVE, 0, 1, AttnParams>(p);
 }
 
 // The same kernel over a bounded view of the prefix.
-template <int D, int NWAVE, int VIEW>
-__global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(2))) void slot_view_bf16_kernel(ViewParams p) {
-  attn_bf16_body<D, NWAVE, VIEW, ViewParams>(p);
+template <int D, int NWAVE, int VIEW, int GRP>
+__global__ __launch_bounds__(NWAVE * GRP * 64) __attribute__((amdgpu_waves_per_eu(2))) void slot_view_bf16_kernel(
+    ViewParams p) {
+  attn_bf16_body<D, NWAVE, VIEW, GRP, ViewParams>(p);
 }
 
 // Exact merge of the prefix splits: O = sum_i w_i O_i / sum_i w_i with
@@ -1097,9 +1148,11 @@ template <int D, int VIEW>
 void launch_view_as(const ViewParams& all, hipStream_t stream) {
   for_each_view_launch(all, [&](const ViewParams& p) {
     if (p.rows_per_block == kAttnWideRowsPerBlock) {
-      slot_view_bf16_kernel<D, 8, VIEW><<<dim3(8 * p.per_xcd), dim3(512), 0, stream>>>(p);
+      slot_view_bf16_kernel<D, 8, VIEW, 1><<<dim3(8 * p.per_xcd), dim3(512), 0, stream>>>(p);
+    } else if (p.key_groups == 2) {
+      slot_view_bf16_kernel<D, 4, VIEW, 2><<<dim3(8 * p.per_xcd), dim3(512), 0, stream>>>(p);
     } else {
-      slot_view_bf16_kernel<D, 4, VIEW><<<dim3(8 * p.per_xcd), dim3(256), 0, stream>>>(p);
+      slot_view_bf16_kernel<D, 4, VIEW, 1><<<dim3(8 * p.per_xcd), dim3(256), 0, stream>>>(p);
     }
   });
 }

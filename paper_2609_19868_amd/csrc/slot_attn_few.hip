@@ -31,8 +31,26 @@ namespace zarya {
 namespace {
 
 constexpr int FKT = 32;     // keys per tile
-constexpr int FNW = 4;      // waves per workgroup
+constexpr int NW = 4;       // waves per workgroup
 constexpr float kRescaleLog2 = 8.f;  // growth of a row maximum (log2 units) that forces a rescale
+
+// LDS reads issued where they stand, valid after a matching lds_wait and tie
+template <int OFF>
+__device__ __forceinline__ uint32_t lds_read_b32(uint32_t addr) {
+  uint32_t r;
+  asm volatile("ds_read_b32 %0, %1 offset:%2" : "=v"(r) : "v"(addr), "i"(OFF));
+  return r;
+}
+template <int OFF>
+__device__ __forceinline__ uint32_t lds_read_u8(uint32_t addr) {
+  uint32_t r;
+  asm volatile("ds_read_u8 %0, %1 offset:%2" : "=v"(r) : "v"(addr), "i"(OFF));
+  return r;
+}
+__device__ __forceinline__ void lds_tie(uint32_t& x) { asm volatile("" : "+v"(x)); }
+
+// four words at an even address (global accesses need no more)
+typedef uint32_t u32x4_a2 __attribute__((ext_vector_type(4), aligned(2)));
 
 __device__ __forceinline__ f32x4 mfma16x16x32(const bf16x8& a, const bf16x8& b, const f32x4& c) {
   return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a, b, c, 0, 0, 0);
@@ -55,8 +73,8 @@ struct FewRaw<D, true> {
   static constexpr int KW = D / 32;  // words of codes per K quarter row
   uint32_t k[2][KW];
   uint32_t ks[2];
-  uint32_t v[8];   // D/16 codes of each of eight keys
-  uint32_t vs[8];  // a key's scales, the lane's own in the low byte (D = 64: 16-bit pieces)
+  uint32_t v[8];        // D/16 codes of each of eight keys
+  uint32_t vs[D / 16];  // the eight keys' scales, D/32 bytes a key
 };
 
 template <int D>
@@ -66,13 +84,25 @@ struct FewRaw<D, false> {
 };
 
 template <int D, int NT, bool Q4>
-__global__ __launch_bounds__(FNW * 64) __attribute__((amdgpu_waves_per_eu(2))) void slot_view_few_kernel(ViewParams p) {
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void slot_view_few_kernel(
+    ViewParams p) {
   constexpr int RB = 16 * NT;
   constexpr int NKS = D / 32;  // k-steps of the QK^T contraction
   constexpr int NOB = D / 16;  // 16-wide blocks of the output = elements of a V row per lane
   constexpr int OSTR = D + 4;  // row stride of the partial outputs in LDS
-  __shared__ __attribute__((aligned(16))) float part_o[FNW][RB][OSTR];
-  __shared__ float part_m[FNW][RB], part_l[FNW][RB];
+  // 4-bit codes at D = 128 come through LDS: a ring of tiles for each wave (the codes
+  // of K, of V, and both scales), requested RING - 1 tiles ahead, so that what is on
+  // its way takes no registers.  Key k of a tile is row (k % 8) * 4 + k / 8, and a
+  // row's 16-byte pieces are swapped by bits 2 and 3 of that: both the quarter
+  // rows that a lane takes of K and the words of V fall on distinct banks.
+  constexpr bool Ring = Q4 && D == 128;
+  constexpr int RING = NT == 1 ? 3 : 4;
+  constexpr int TILE = FKT * (D + 2 * (D / 32));
+  constexpr int PART = NW * RB * OSTR * 4;
+  constexpr int LDS = Ring && NW * RING * TILE > PART ? NW * RING * TILE : PART;
+  __shared__ __attribute__((aligned(16))) uint8_t lds[LDS];  // the rings, then the partial outputs
+  auto part_o = reinterpret_cast<float(*)[RB][OSTR]>(lds);
+  __shared__ float part_m[NW][RB], part_l[NW][RB];
 
   int w = xcd_work_index(blockIdx.x, p.per_xcd, p.n_items);
   if (w < 0) return;
@@ -94,7 +124,6 @@ __global__ __launch_bounds__(FNW * 64) __attribute__((amdgpu_waves_per_eu(2))) v
   // first, the draft tokens' after them
   const int per_split = (tiles.nt + p.n_split - 1) / p.n_split;
   const int first = min(split * per_split, tiles.nt), end = min(tiles.nt, first + per_split);
-  const int pre_end = min(end, tiles.n_pre);
 
   // the lane's rows: visible draft keys, and the first draft key inside the window
   int vis_lo[NT], vis_hi[NT], win_lo[NT];
@@ -123,12 +152,14 @@ __global__ __launch_bounds__(FNW * 64) __attribute__((amdgpu_waves_per_eu(2))) v
   }
   const float c2 = p.scale_log2;
   const int ka = 8 * (n >> 2) + (n & 3);  // the tile's key in row n of product a
+  const uint32_t vs_rot = 8 * (n * (D / 16) / 32) + 9;  // rotation of a key's scales that puts the lane's at bit 23
 
   // K and V of one tile -> registers.  Keys past the last one follow it (their
-  // scores are masked); whole tiles need no such care.
-  auto fetch = [&](auto& raw, bool pre, int key0) __attribute__((always_inline)) {
+  // scores are masked); whole tiles need no such care, and a lane's loads are one
+  // address and constants.
+  auto fetch = [&](auto& raw, bool pre, int key0, auto whole_tile) __attribute__((always_inline)) {
+    constexpr bool whole = decltype(whole_tile)::value;
     const int last = (pre ? Pb : p.T) - 1 - key0;
-    const bool whole = last >= FKT - 1;
     auto at = [&](int k) { return whole ? k : min(k, last); };
     if constexpr (std::is_same_v<std::decay_t<decltype(raw)>, FewRaw<D, true>>) {
       const size_t base = (size_t)bg * p.C + key0;
@@ -152,7 +183,25 @@ __global__ __launch_bounds__(FNW * 64) __attribute__((amdgpu_waves_per_eu(2))) v
         } else {
           raw.v[j] = *reinterpret_cast<const uint16_t*>(vc + k * (D / 2) + n * 2);
         }
-        raw.vs[j] = vscale[k * (D / 32) + n * (D / 16) / 32];
+      }
+      if constexpr (whole) {
+#pragma unroll
+        for (int e = 0; e < D / 64; ++e) {
+          const u32x4_a2 x = *reinterpret_cast<const u32x4_a2*>(vscale + 8 * q4 * (D / 32) + 16 * e);
+#pragma unroll
+          for (int c = 0; c < 4; ++c) raw.vs[4 * e + c] = x[c];
+        }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+          const uint8_t* src = vscale + (uint32_t)at(8 * q4 + j) * (D / 32);
+          if constexpr (D == 128) {
+            raw.vs[j] = *reinterpret_cast<const uint32_t*>(src);
+          } else {
+            const uint32_t x = *reinterpret_cast<const uint16_t*>(src);
+            raw.vs[j / 2] = j & 1 ? raw.vs[j / 2] | x << 16 : x;
+          }
+        }
       }
     } else {
       const size_t base = pre ? (size_t)bg * p.C + key0 : (size_t)bg * p.T + key0;
@@ -178,7 +227,16 @@ __global__ __launch_bounds__(FNW * 64) __attribute__((amdgpu_waves_per_eu(2))) v
   };
 
   // scores, online softmax and value products of one tile
-  auto compute = [&](const auto& raw, bool pre, int key0) __attribute__((always_inline)) {
+  auto compute = [&](auto& raw, bool pre, int key0, auto ring) __attribute__((always_inline)) {
+    if constexpr (decltype(ring)::value) {
+      lds_wait<10>();  // K's codes and scales
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        lds_tie(raw.ks[t]);
+#pragma unroll
+        for (int e = 0; e < D / 32; ++e) lds_tie(raw.k[t][e]);
+      }
+    }
     constexpr bool Codes = std::is_same_v<std::decay_t<decltype(raw)>, FewRaw<D, true>>;
     f32x4 s[NT][2];
 #pragma unroll
@@ -242,11 +300,26 @@ __global__ __launch_bounds__(FNW * 64) __attribute__((amdgpu_waves_per_eu(2))) v
       }
       pb[r] = __builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3]));
     }
+    if constexpr (decltype(ring)::value) {
+      lds_wait<0>();
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        lds_tie(raw.v[j]);
+        lds_tie(raw.vs[j]);
+      }
+    }
     // element pair (2e, 2e + 1) of the lane's part of key j's V row, as packed bf16
     float vsc[8];
     if constexpr (Codes) {
 #pragma unroll
-      for (int j = 0; j < 8; ++j) vsc[j] = q4_scale(raw.vs[j]);
+      for (int j = 0; j < 8; ++j) {
+        // the lane's scale byte rotated into the exponent field
+        if constexpr (D == 128) {
+          vsc[j] = __uint_as_float(__builtin_amdgcn_alignbit(raw.vs[j], raw.vs[j], vs_rot));
+        } else {
+          vsc[j] = __uint_as_float(__builtin_amdgcn_alignbit(raw.vs[j / 2], raw.vs[j / 2], vs_rot + 16 * (j & 1)));
+        }
+      }
     }
 #pragma unroll
     for (int e = 0; e < NOB / 2; ++e) {
@@ -280,32 +353,135 @@ __global__ __launch_bounds__(FNW * 64) __attribute__((amdgpu_waves_per_eu(2))) v
     }
   };
 
-  if constexpr (!Q4 && D == 128 && NT == 2) {  // no registers left to read ahead
-    for (int i = first + wave; i < pre_end; i += FNW) {
-      FewRaw<D, false> raw;
-      fetch(raw, true, tiles.key0(i));
-      compute(raw, true, tiles.key0(i));
+  constexpr std::true_type yes{};
+  constexpr std::false_type no{};
+  int i = first + wave;
+  if constexpr (Ring) {
+    // the prefix's tiles
+    const int pre_end = min(end, tiles.n_pre);
+    uint8_t* const ring = lds + wave * RING * TILE;
+    const int row = lane >> 2;  // rows 0..15 of a tile by the first load, 16..31 by the second
+    const int key_of = (row & 3) * 8 + (row >> 2);  // of the row; 4 more in the second half
+    const uint32_t piece = 16 * ((lane & 3) ^ ((row >> 2) & 3));
+    // lanes 0..31 load K's scales, the others V's (the two pointers as values: choosing
+    // between the arguments themselves would be a load in each request)
+    uint64_t ks_base = reinterpret_cast<uint64_t>(p.k_scale), vs_base = reinterpret_cast<uint64_t>(p.v_scale);
+    asm("" : "+s"(ks_base), "+s"(vs_base));
+    const uint8_t* const scales = reinterpret_cast<const uint8_t*>(lane < 32 ? ks_base : vs_base);
+    auto request = [&](int tile, int slot) __attribute__((always_inline)) {
+      const int key0 = tiles.key0(tile), last = Pb - 1 - key0;
+      const size_t base = (size_t)bg * p.C + key0;
+      const uint8_t* kc = reinterpret_cast<const uint8_t*>(p.k_cache) + base * (D / 2);
+      const uint8_t* vc = reinterpret_cast<const uint8_t*>(p.v_cache) + base * (D / 2);
+      const uint8_t* sc = scales + base * (D / 32);
+      int a = key_of, b = key_of + 4, c = lane & 31;
+      if (last < FKT - 1) {  // keys past the last one follow it (their scores are masked)
+        a = min(a, last);
+        b = min(b, last);
+        c = min(c, last);
+      }
+      uint8_t* dst = ring + slot * TILE;
+      dma16(kc + (uint32_t)(a * (D / 2) + piece), dst);
+      dma16(kc + (uint32_t)(b * (D / 2) + piece), dst + 1024);
+      dma16(vc + (uint32_t)(a * (D / 2) + piece), dst + 2048);
+      dma16(vc + (uint32_t)(b * (D / 2) + piece), dst + 3072);
+      dma4(sc + (uint32_t)(c * (D / 32)), dst + 4096);
+    };
+    constexpr int OPS = 5;  // loads of a tile
+    const uint32_t lane0 = lds_addr(ring);
+    // K: rows of keys ka and ka + 4, (n & 3) * 4 + (n >> 2) and 16 more, piece q4
+    const uint32_t k_at = ((n & 3) * 4 + (n >> 2)) * (D / 2) + 16 * (q4 ^ (n & 3));
+    const uint32_t ks_at = 4096 + ka * (D / 32) + q4;
+    // V: row j * 4 + q4 of key 8 * q4 + j, word n % 4 of piece (n / 4) ^ (j % 4)
+    const uint32_t v_at = 2048 + q4 * (D / 2) + 4 * (n & 3);
+    const uint32_t vs_at = 4096 + 128 + 32 * q4;
+#pragma unroll
+    for (int a = 0; a < RING - 1; ++a)
+      if (i + a * NW < pre_end) request(i + a * NW, a);
+    // the queries are waited for here: in the loop it would be with every tile's loads
+#pragma unroll
+    for (int r = 0; r < NT; ++r)
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) lds_tie(qf[r][ks]);
+    int slot = 0;
+    for (; i < pre_end; i += NW) {
+      const int ahead = i + (RING - 1) * NW;
+      if (ahead < pre_end) {
+        request(ahead, slot == 0 ? RING - 1 : slot - 1);
+        wait_vmcnt<(RING - 1) * OPS>();
+      } else {
+        wait_vmcnt<0>();
+      }
+      const uint32_t at = lane0 + slot * TILE;
+      FewRaw<D, true> raw;
+      auto quarter = [&](uint32_t (&dst)[4], const bf16x8& x) __attribute__((always_inline)) {
+        const uint4 w = __builtin_bit_cast(uint4, x);
+        dst[0] = w.x;
+        dst[1] = w.y;
+        dst[2] = w.z;
+        dst[3] = w.w;
+      };
+      const bf16x8 k0 = lds_read_b128<0>(at + k_at), k1 = lds_read_b128<1024>(at + k_at);
+      raw.ks[0] = lds_read_u8<0>(at + ks_at);
+      raw.ks[1] = lds_read_u8<4 * (D / 32)>(at + ks_at);
+      quarter(raw.k[0], k0);
+      quarter(raw.k[1], k1);
+      uint32_t va[4];
+#pragma unroll
+      for (int j = 0; j < 4; ++j) va[j] = at + v_at + 16 * ((n >> 2) ^ j);
+      raw.v[0] = lds_read_b32<0>(va[0]);
+      raw.v[1] = lds_read_b32<4 * (D / 2)>(va[1]);
+      raw.v[2] = lds_read_b32<8 * (D / 2)>(va[2]);
+      raw.v[3] = lds_read_b32<12 * (D / 2)>(va[3]);
+      raw.v[4] = lds_read_b32<16 * (D / 2)>(va[0]);
+      raw.v[5] = lds_read_b32<20 * (D / 2)>(va[1]);
+      raw.v[6] = lds_read_b32<24 * (D / 2)>(va[2]);
+      raw.v[7] = lds_read_b32<28 * (D / 2)>(va[3]);
+      const bf16x8 s0 = lds_read_b128<0>(at + vs_at), s1 = lds_read_b128<16>(at + vs_at);
+      const uint4 w0 = __builtin_bit_cast(uint4, s0), w1 = __builtin_bit_cast(uint4, s1);
+      const uint32_t w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+#pragma unroll
+      for (int j = 0; j < 8; ++j) raw.vs[j] = w[j];
+      compute(raw, true, tiles.key0(i), yes);
+      slot = slot == RING - 1 ? 0 : slot + 1;
     }
   } else {
-    FewRaw<D, Q4> raw[2];
-    int i = first + wave;
-    if (i < pre_end) fetch(raw[0], true, tiles.key0(i));
-    while (i < pre_end) {
-      if (i + FNW < pre_end) fetch(raw[1], true, tiles.key0(i + FNW));
-      compute(raw[0], true, tiles.key0(i));
-      i += FNW;
-      if (i >= pre_end) break;
-      if (i + FNW < pre_end) fetch(raw[0], true, tiles.key0(i + FNW));
-      compute(raw[1], true, tiles.key0(i));
-      i += FNW;
+    // the prefix's whole tiles
+    const int whole_end = min(end, tiles.n_pre - (Pb % FKT != 0));
+    if constexpr (!Q4 && D == 128 && NT == 2) {  // no registers left to read ahead
+      for (; i < whole_end; i += NW) {
+        FewRaw<D, false> raw;
+        fetch(raw, true, tiles.key0(i), yes);
+        compute(raw, true, tiles.key0(i), no);
+      }
+    } else {
+      FewRaw<D, Q4> raw[2];
+      if (i < whole_end) fetch(raw[0], true, tiles.key0(i), yes);
+      while (i < whole_end) {
+        if (i + NW < whole_end) fetch(raw[1], true, tiles.key0(i + NW), yes);
+        compute(raw[0], true, tiles.key0(i), no);
+        i += NW;
+        if (i >= whole_end) break;
+        if (i + NW < whole_end) fetch(raw[0], true, tiles.key0(i + NW), yes);
+        compute(raw[1], true, tiles.key0(i), no);
+        i += NW;
+      }
     }
   }
-  // the draft tokens' tiles go round from the wave after the prefix's last one
-  for (int i = max(first, tiles.n_pre) + ((wave + FNW - (max(first, tiles.n_pre) - first) % FNW) & (FNW - 1)); i < end;
-       i += FNW) {
+  // its last one where it is not whole, and the draft tokens' tiles
+  for (; i < end; i += NW) {
+    const bool pre = i < tiles.n_pre;
+    if constexpr (Q4 && !Ring) {
+      if (pre) {
+        FewRaw<D, true> raw;
+        fetch(raw, true, tiles.key0(i), no);
+        compute(raw, true, tiles.key0(i), no);
+        continue;
+      }
+    }
     FewRaw<D, false> raw;
-    fetch(raw, false, tiles.key0(i));
-    compute(raw, false, tiles.key0(i));
+    fetch(raw, pre, tiles.key0(i), no);
+    compute(raw, pre, tiles.key0(i), no);
   }
 
   // ---- values that are not finite: as in attn_bf16_body, the wave's sums once
@@ -334,7 +510,7 @@ __global__ __launch_bounds__(FNW * 64) __attribute__((amdgpu_waves_per_eu(2))) v
         return *reinterpret_cast<const bf16x8*>(base + ((size_t)bg * (pre ? p.C : p.T) + key) * D + d);
       };
 #pragma unroll 1
-      for (int i = first + wave; i < end; i += FNW) {
+      for (i = first + wave; i < end; i += NW) {
         const bool pre = i < tiles.n_pre;
         const int key0 = tiles.key0(i), kend = min(key0 + FKT, pre ? Pb : p.T), off = pre ? Pb : 0;
 #pragma unroll 1
@@ -373,6 +549,7 @@ __global__ __launch_bounds__(FNW * 64) __attribute__((amdgpu_waves_per_eu(2))) v
   }
 
   // ---- merge of the waves' partials, in wave order
+  if constexpr (Ring) __syncthreads();  // the rings give way to them
 #pragma unroll
   for (int r = 0; r < NT; ++r) {
     l[r] += __shfl_xor(l[r], 16);
@@ -390,17 +567,17 @@ __global__ __launch_bounds__(FNW * 64) __attribute__((amdgpu_waves_per_eu(2))) v
             f32x4{oacc[r][ob][v], oacc[r][ob + 1][v], oacc[r][ob + 2][v], oacc[r][ob + 3][v]};
   }
   __syncthreads();
-  for (int x = threadIdx.x; x < RB * (D / 4); x += FNW * 64) {
+  for (int x = threadIdx.x; x < RB * (D / 4); x += NW * 64) {
     const int lr = x / (D / 4), c = 4 * (x % (D / 4));
     const int row = rb * RB + lr;
     if (row >= p.R) break;
     float mx = part_m[0][lr];
 #pragma unroll
-    for (int i = 1; i < FNW; ++i) mx = fmaxf(mx, part_m[i][lr]);
+    for (int i = 1; i < NW; ++i) mx = fmaxf(mx, part_m[i][lr]);
     float lt = 0.f;
     f32x4 o{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-    for (int i = 0; i < FNW; ++i) {
+    for (int i = 0; i < NW; ++i) {
       const float sc = fast_exp2((part_m[i][lr] - mx) * c2);  // 0 for a wave without a visible key
       lt += sc * part_l[i][lr];
       o += sc * *reinterpret_cast<const f32x4*>(&part_o[i][lr][c]);
@@ -424,9 +601,9 @@ template <int D, bool Q4>
 static void launch_few_as(const ViewParams& all, hipStream_t stream) {
   for_each_view_launch(all, [&](const ViewParams& p) {
     if (p.rows_per_block == 16) {
-      slot_view_few_kernel<D, 1, Q4><<<dim3(8 * p.per_xcd), dim3(FNW * 64), 0, stream>>>(p);
+      slot_view_few_kernel<D, 1, Q4><<<dim3(8 * p.per_xcd), dim3(NW * 64), 0, stream>>>(p);
     } else {
-      slot_view_few_kernel<D, 2, Q4><<<dim3(8 * p.per_xcd), dim3(FNW * 64), 0, stream>>>(p);
+      slot_view_few_kernel<D, 2, Q4><<<dim3(8 * p.per_xcd), dim3(NW * 64), 0, stream>>>(p);
     }
   });
 }
