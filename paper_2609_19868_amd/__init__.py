@@ -152,12 +152,45 @@ def slot_attn_desc(q, k_cache, k_slot, n_slots, slot_len, pass_=PASS_DIFFUSION, 
     P = C if prefix_len is None else int(prefix_len)
     if q.dtype not in _DT:
         raise ValueError(f"unsupported dtype {q.dtype}")
+    # in the order of the structure's fields (by name it takes twice as long)
     return _lib.SlotAttnDesc(
-        batch=B, n_q_heads=Hq, n_kv_heads=Hkv, head_dim=D, prefix_len=P, kv_capacity=C,
-        n_slots=int(n_slots), slot_len=int(slot_len),
-        softmax_scale=float(1.0 / math.sqrt(D) if softmax_scale is None else softmax_scale),
-        pass_=int(pass_), cross_slot=int(cross_slot), dtype=_DT[q.dtype], prefix_splits=int(prefix_splits),
+        B, Hq, Hkv, D, P, C, int(n_slots), int(slot_len),
+        float(1.0 / math.sqrt(D) if softmax_scale is None else softmax_scale),
+        int(pass_), int(cross_slot), _DT[q.dtype], int(prefix_splits),
     )
+
+
+def _attn_tensors(q, k_slot, v_slot, n_slots, slot_pass, prefix_lens, out, lse, want_lse):
+    """The tensors of an attention call other than its cache, checked; (out, lse),
+    allocated where they are not given."""
+    B, Hq, T, D = q.shape
+    dev, dt = q.device, q.dtype
+    kv_shape = (B, k_slot.shape[1], T, D)
+    if out is None:
+        out = torch.empty((B, Hq, T, D), dtype=dt, device=dev)
+    if lse is None and want_lse:
+        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=dev)
+    # one expression for the usual call (2 us; tensor by tensor 4), which _need says
+    # more about when it does not hold
+    if not (
+        dev.type == "cuda" and q.is_contiguous()
+        and k_slot.dtype is dt and k_slot.shape == kv_shape and k_slot.device == dev and k_slot.is_contiguous()
+        and v_slot.dtype is dt and v_slot.shape == kv_shape and v_slot.device == dev and v_slot.is_contiguous()
+        and out.dtype is dt and out.shape == q.shape and out.device == dev and out.is_contiguous()
+        and (lse is None or (lse.dtype is torch.float32 and lse.shape == (B, Hq, T) and lse.device == dev
+                             and lse.is_contiguous()))
+        and (prefix_lens is None or (prefix_lens.dtype is torch.int32 and prefix_lens.shape == (B,)
+                                     and prefix_lens.device == dev and prefix_lens.is_contiguous()))
+        and slot_pass is None
+    ):
+        _need(q, "q", (B, Hq, T, D), dt, dev)
+        _need(k_slot, "k_slot", kv_shape, dt, dev)
+        _need(v_slot, "v_slot", kv_shape, dt, dev)
+        _need_opt(slot_pass, "slot_pass", (B, n_slots), torch.uint8, dev)
+        _need_opt(prefix_lens, "prefix_lens", (B,), torch.int32, dev)
+        _need(out, "out", (B, Hq, T, D), dt, dev)
+        _need_opt(lse, "lse", (B, Hq, T), torch.float32, dev)
+    return out, lse
 
 
 def slot_attn(q, k_cache, v_cache, k_slot, v_slot, n_slots, slot_len, pass_=PASS_DIFFUSION,
@@ -180,23 +213,10 @@ def slot_attn(q, k_cache, v_cache, k_slot, v_slot, n_slots, slot_len, pass_=PASS
     Hkv = k_slot.shape[1]
     desc = slot_attn_desc(q, k_cache, k_slot, n_slots, slot_len, pass_, cross_slot, prefix_len, softmax_scale,
                           prefix_splits)
-    _need(q, "q", (B, Hq, T, D), dt, dev)
-    _need(k_slot, "k_slot", (B, Hkv, T, D), dt, dev)
-    _need(v_slot, "v_slot", (B, Hkv, T, D), dt, dev)
+    out, lse = _attn_tensors(q, k_slot, v_slot, n_slots, slot_pass, prefix_lens, out, lse, want_lse)
     if k_cache is not None:
         _need(k_cache, "k_cache", (B, Hkv, desc.kv_capacity, D), dt, dev)
         _need(v_cache, "v_cache", (B, Hkv, desc.kv_capacity, D), dt, dev)
-    if slot_pass is not None:
-        _need(slot_pass, "slot_pass", (B, n_slots), torch.uint8, dev)
-    if prefix_lens is not None:
-        _need(prefix_lens, "prefix_lens", (B,), torch.int32, dev)
-    if out is None:
-        out = torch.empty((B, Hq, T, D), dtype=dt, device=dev)
-    _need(out, "out", (B, Hq, T, D), dt, dev)
-    if lse is None and want_lse:
-        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=dev)
-    if lse is not None:
-        _need(lse, "lse", (B, Hq, T), torch.float32, dev)
     win = _window(window, sinks)
     ws_bytes = _lib.slot_attn_workspace_size(desc) if win is None else _lib.slot_attn_window_workspace_size(desc, win)
     _need_workspace(workspace, ws_bytes, dev)
@@ -231,14 +251,28 @@ def q4_cache(batch, n_kv_heads, capacity, head_dim, device="cuda"):
 
 def _need_q4(cache, device):
     """(B, Hkv, C, D) of a cache whose four arrays fit together and are on `device`."""
-    if cache.k.dim() != 4:
-        raise ValueError(f"cache.k: expected 4 dimensions, got {tuple(cache.k.shape)}")
-    B, Hkv, C, half = cache.k.shape
-    _need(cache.k, "cache.k", (B, Hkv, C, half), torch.uint8, device)
-    _need(cache.v, "cache.v", (B, Hkv, C, half), torch.uint8, device)
-    _need(cache.k_scale, "cache.k_scale", (B, Hkv, C, half // 16), torch.uint8, device)
-    _need(cache.v_scale, "cache.v_scale", (B, Hkv, C, half // 16), torch.uint8, device)
+    k, k_scale, v, v_scale = cache
+    if k.dim() != 4:
+        raise ValueError(f"cache.k: expected 4 dimensions, got {tuple(k.shape)}")
+    B, Hkv, C, half = codes = tuple(k.shape)
+    scales = (B, Hkv, C, half // 16)
+    u8 = torch.uint8
+    if not (
+        device.type == "cuda" and k.dtype is u8 and k.device == device and k.is_contiguous()
+        and v.dtype is u8 and v.shape == codes and v.device == device and v.is_contiguous()
+        and k_scale.dtype is u8 and k_scale.shape == scales and k_scale.device == device and k_scale.is_contiguous()
+        and v_scale.dtype is u8 and v_scale.shape == scales and v_scale.device == device and v_scale.is_contiguous()
+    ):
+        _need(k, "cache.k", codes, u8, device)
+        _need(k_scale, "cache.k_scale", scales, u8, device)
+        _need(v, "cache.v", codes, u8, device)
+        _need(v_scale, "cache.v_scale", scales, u8, device)
     return B, Hkv, C, 2 * half
+
+
+def _q4_ptrs(cache):
+    k, k_scale, v, v_scale = cache
+    return k.data_ptr(), k_scale.data_ptr(), v.data_ptr(), v_scale.data_ptr()
 
 
 def _window(window, sinks):
@@ -246,7 +280,7 @@ def _window(window, sinks):
         if sinks:
             raise ValueError("sinks need a window")
         return None
-    return _lib.AttnWindow(window=_int32(window, "window"), sinks=_int32(sinks, "sinks"))
+    return _lib.AttnWindow(_int32(window, "window"), _int32(sinks, "sinks"))
 
 
 def _int32(x, name):
@@ -270,29 +304,18 @@ def slot_attn_q4(q, cache, k_slot, v_slot, n_slots, slot_len, pass_=PASS_DIFFUSI
     Hkv = k_slot.shape[1]
     desc = slot_attn_desc(q, cache.k, k_slot, n_slots, slot_len, pass_, cross_slot, prefix_len, softmax_scale,
                           prefix_splits)
-    _need(q, "q", (B, Hq, T, D), dt, dev)
-    _need(k_slot, "k_slot", (B, Hkv, T, D), dt, dev)
-    _need(v_slot, "v_slot", (B, Hkv, T, D), dt, dev)
+    out, lse = _attn_tensors(q, k_slot, v_slot, n_slots, slot_pass, prefix_lens, out, lse, want_lse)
     shape = _need_q4(cache, dev)
     if shape != (B, Hkv, desc.kv_capacity, D):
         raise ValueError(f"cache: expected batch, heads and head size {(B, Hkv, D)}, got {(shape[0], shape[1], shape[3])}")
-    _need_opt(slot_pass, "slot_pass", (B, n_slots), torch.uint8, dev)
-    _need_opt(prefix_lens, "prefix_lens", (B,), torch.int32, dev)
-    if out is None:
-        out = torch.empty((B, Hq, T, D), dtype=dt, device=dev)
-    _need(out, "out", (B, Hq, T, D), dt, dev)
-    if lse is None and want_lse:
-        lse = torch.empty((B, Hq, T), dtype=torch.float32, device=dev)
-    _need_opt(lse, "lse", (B, Hq, T), torch.float32, dev)
     win = _window(window, sinks)
     ws_bytes = _lib.slot_attn_q4_workspace_size(desc, win)
     _need_workspace(workspace, ws_bytes, dev)
     if workspace is None and ws_bytes > 0:
         workspace = torch.empty(ws_bytes, dtype=torch.uint8, device=dev)
-    _call(_lib.lib().zarya_slot_attn_q4, dev, ctypes.byref(desc), None if win is None else ctypes.byref(win), _ptr(q),
-          _ptr(cache.k), _ptr(cache.k_scale), _ptr(cache.v), _ptr(cache.v_scale), _ptr(k_slot), _ptr(v_slot),
-          _ptr(slot_pass), _ptr(prefix_lens), _ptr(out), _ptr(lse), _ptr(workspace),
-          0 if workspace is None else workspace.numel())
+    _call(_lib.lib().zarya_slot_attn_q4, dev, ctypes.byref(desc), None if win is None else ctypes.byref(win),
+          q.data_ptr(), *_q4_ptrs(cache), k_slot.data_ptr(), v_slot.data_ptr(), _ptr(slot_pass), _ptr(prefix_lens),
+          out.data_ptr(), _ptr(lse), _ptr(workspace), 0 if workspace is None else workspace.numel())
     return out, lse
 
 
@@ -505,9 +528,9 @@ def kv_quantize(k, v, cache, starts=None, lens=None):
     _need(v, "v", (B, Hkv, N, D), dt, dev)
     _need_opt(starts, "starts", (B,), torch.int32, dev)
     _need_opt(lens, "lens", (B,), torch.int32, dev)
-    desc = _lib.KvQ4Desc(batch=B, n_kv_heads=Hkv, head_dim=D, kv_capacity=C, n_rows=N, dtype=_DT[dt])
-    _call(_lib.lib().zarya_kv_quantize, dev, ctypes.byref(desc), _ptr(k), _ptr(v), _ptr(starts), _ptr(lens),
-          _ptr(cache.k), _ptr(cache.k_scale), _ptr(cache.v), _ptr(cache.v_scale))
+    desc = _lib.KvQ4Desc(B, Hkv, D, C, N, _DT[dt])
+    _call(_lib.lib().zarya_kv_quantize, dev, ctypes.byref(desc), k.data_ptr(), v.data_ptr(), _ptr(starts), _ptr(lens),
+          *_q4_ptrs(cache))
     return cache
 
 
@@ -526,13 +549,15 @@ def kv_dequantize(cache, n_rows=None, dtype=torch.bfloat16, lens=None, out=None)
         raise ValueError(f"n_rows: {N} is not in [0, {C}]")
     _need_opt(lens, "lens", (B,), torch.int32, dev)
     if out is None:
-        out = tuple(torch.empty((B, Hkv, N, D), dtype=dtype, device=dev) for _ in range(2))
-    k, v = out
-    _need(k, "out[0] (k)", (B, Hkv, N, D), dtype, dev)
-    _need(v, "out[1] (v)", (B, Hkv, N, D), dtype, dev)
-    desc = _lib.KvQ4Desc(batch=B, n_kv_heads=Hkv, head_dim=D, kv_capacity=C, n_rows=N, dtype=_DT[dtype])
-    _call(_lib.lib().zarya_kv_dequantize, dev, ctypes.byref(desc), _ptr(cache.k), _ptr(cache.k_scale), _ptr(cache.v),
-          _ptr(cache.v_scale), _ptr(lens), _ptr(k), _ptr(v))
+        k = torch.empty((B, Hkv, N, D), dtype=dtype, device=dev)
+        v = torch.empty((B, Hkv, N, D), dtype=dtype, device=dev)
+    else:
+        k, v = out
+        _need(k, "out[0] (k)", (B, Hkv, N, D), dtype, dev)
+        _need(v, "out[1] (v)", (B, Hkv, N, D), dtype, dev)
+    desc = _lib.KvQ4Desc(B, Hkv, D, C, N, _DT[dtype])
+    _call(_lib.lib().zarya_kv_dequantize, dev, ctypes.byref(desc), *_q4_ptrs(cache), _ptr(lens), k.data_ptr(),
+          v.data_ptr())
     return k, v
 
 
@@ -553,8 +578,7 @@ def kv_append_q4(cache, prefix_lens, k_slot, v_slot, accepted, order):
     _need(accepted, "accepted", (B, S, L), torch.uint8, dev)
     _need(order, "order", (B, S), torch.int32, dev)
     _need(prefix_lens, "prefix_lens", (B,), torch.int32, dev)
-    desc = _lib.KvAppendDesc(batch=B, n_kv_heads=Hkv, head_dim=D, kv_capacity=C, n_slots=S, slot_len=L,
-                             dtype=_DT[dt])
-    _call(_lib.lib().zarya_kv_append_q4, dev, ctypes.byref(desc), _ptr(k_slot), _ptr(v_slot), _ptr(accepted),
-          _ptr(order), _ptr(prefix_lens), _ptr(cache.k), _ptr(cache.k_scale), _ptr(cache.v), _ptr(cache.v_scale))
+    desc = _lib.KvAppendDesc(B, Hkv, D, C, S, L, _DT[dt])
+    _call(_lib.lib().zarya_kv_append_q4, dev, ctypes.byref(desc), k_slot.data_ptr(), v_slot.data_ptr(),
+          accepted.data_ptr(), order.data_ptr(), prefix_lens.data_ptr(), *_q4_ptrs(cache))
     return cache, prefix_lens
