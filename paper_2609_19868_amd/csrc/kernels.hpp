@@ -174,7 +174,13 @@ struct KvQ4Params {
 struct AppendQ4Params : AppendParams {
   int D, bf16;
   Q4CachePtrs cache;  // instead of k_cache and v_cache
+  int copies, counts;  // this launch fills the cache; moves the prefix lengths (set by the launcher)
 };
+// Pieces of eight elements, K's and V's of all draft tokens of a row, that one
+// workgroup takes, and beyond that each of several (8 heads, D = 128, a third of the
+// tokens accepted and all: 64 tokens in one launch 9.0 and 11.3 us, in two 9.5 and
+// 10.1; 128 9.3 and 18.7, 9.1 and 10.1; 4096, all, 497 and 20.5).
+constexpr int64_t kAppendQ4OneWG = 16384, kAppendQ4PartPieces = 4096;
 
 // Mode A reveal: one workgroup per batch row sorts the row's N keys in LDS.
 struct RevealParams {

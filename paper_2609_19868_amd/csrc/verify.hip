@@ -95,8 +95,8 @@ __global__ __launch_bounds__(MAXT) void verify_accept_kernel(AcceptParams p) {
 // and move the row's prefix length.  `lg`: log2 of the lanes per slot.
 // B = 16, 8 heads, 4 of 8 slots with 7 of 8 tokens: 9.4 -> 7.2 us (256 threads,
 // a serial scan over the slots and a thread per slot reading its flags).
-// Q4: into the 4-bit cache, eight elements a lane.
-template <bool Q4, class Params>
+// Q4: into the 4-bit cache, eight elements a lane, of bf16 or float32 K/V.
+template <bool Q4, bool BF16, class Params>
 __device__ __forceinline__ void kv_append_body(const Params& p, int lg) {
   __shared__ int slot_of[1024];   // order position -> slot id (or -1)
   __shared__ int count_of[1024];  // order position -> accepted tokens of that slot
@@ -167,20 +167,35 @@ __device__ __forceinline__ void kv_append_body(const Params& p, int lg) {
   each_accepted([&](int i, int token, int rank) { tokens[start_of[i] + rank] = token; }, [](int, int) {});
   __syncthreads();
   if constexpr (Q4) {
-    const int lp = __builtin_ctz(p.D / 8);
-    const int total = (p.Hkv * n) << lp;  // a multiple of 4: the lanes of a block run together
-    for (int e = tid; e < total; e += kThreads) {
-      const int x = e >> lp, c = e & ((1 << lp) - 1);
-      const int g = x / n, i = x - g * n;
-      const size_t src = (((size_t)b * p.Hkv + g) * T + tokens[i]) * p.D + 8 * c;
-      const size_t dst = ((size_t)b * p.Hkv + g) * p.C + p0 + i;
-      float k[8], v[8];
-      load_f32x8(p.k_slot, src, p.bf16, k);
-      load_f32x8(p.v_slot, src, p.bf16, v);
-      store_q4(p.cache.k_codes, p.cache.k_scales, dst, p.D, c, k);
-      store_q4(p.cache.v_codes, p.cache.v_scales, dst, p.D, c, v);
+    // K and V of a head to a wave, or to several where there are more waves than those:
+    // a lane's piece is then found without a division, and its block's base address is
+    // the wave's
+    const int waves = kThreads / 64 * gridDim.y, units = 2 * p.Hkv, per = max(1, waves / units);
+    const int w = blockIdx.y * (kThreads / 64) + __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int lp = __builtin_ctz(p.D / 8), pieces = n << lp;  // a multiple of 4: the lanes of a block run together
+    for (int u = w / per; p.copies && u < units; u += waves / per) {
+      const bool is_v = u & 1;
+      const size_t row0 = (size_t)b * p.Hkv + (u >> 1);
+      const size_t src = row0 * T * p.D, dst = row0 * p.C + p0;
+      const void* from = is_v ? p.v_slot : p.k_slot;
+      uint8_t* codes = is_v ? p.cache.v_codes : p.cache.k_codes;
+      uint8_t* scales = is_v ? p.cache.v_scales : p.cache.k_scales;
+      constexpr int U = 4;  // pieces of a lane whose loads are on their way together
+      for (int e0 = (w % per) * 64 + lane; e0 < pieces; e0 += U * per * 64) {
+        Elements8<BF16> x[U];
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          const int e = min(e0 + k * per * 64, pieces - 4 + (lane & 3));
+          x[k] = load_elements8<BF16, false>(from, src + (uint32_t)(tokens[e >> lp] * p.D + 8 * (e & ((1 << lp) - 1))));
+        }
+#pragma unroll
+        for (int k = 0; k < U; ++k) {
+          const int e = e0 + k * per * 64;
+          if (e < pieces) store_q4<BF16>(codes, scales, dst + (e >> lp), p.D, e & ((1 << lp) - 1), x[k]);
+        }
+      }
     }
-    if (tid == 0) p.prefix_lens[b] = p0 + n;
+    if (tid == 0 && p.counts) p.prefix_lens[b] = p0 + n;
     return;
   }
   const int lp = __builtin_ctz(p.row_bytes / 16);  // 16-byte pieces of a row: 8, 16 or 32
@@ -207,11 +222,12 @@ __device__ __forceinline__ void kv_append_body(const Params& p, int lg) {
 }
 
 __global__ __launch_bounds__(kThreads) void kv_append_kernel(AppendParams p, int lg) {
-  kv_append_body<false, AppendParams>(p, lg);
+  kv_append_body<false, false, AppendParams>(p, lg);
 }
 
+template <bool BF16>
 __global__ __launch_bounds__(kThreads) void kv_append_q4_kernel(AppendQ4Params p, int lg) {
-  kv_append_body<true, AppendQ4Params>(p, lg);
+  kv_append_body<true, BF16, AppendQ4Params>(p, lg);
 }
 
 hipError_t launch_verify_accept(const AcceptParams& p, hipStream_t stream) {
@@ -240,7 +256,22 @@ hipError_t launch_kv_append(const AppendParams& p, hipStream_t stream) {
 }
 
 hipError_t launch_kv_append_q4(const AppendQ4Params& p, hipStream_t stream) {
-  kv_append_q4_kernel<<<dim3(p.B), dim3(kThreads), 0, stream>>>(p, lanes_log2(p.L));
+  // A row's pieces by one workgroup, which also moves its length; of many pieces by
+  // several, after which a second launch moves the lengths that the first reads.
+  AppendQ4Params q = p;
+  q.copies = q.counts = 1;
+  const int64_t pieces = 2LL * p.Hkv * p.S * p.L * (p.D / 8);
+  const auto kernel = p.bf16 ? kv_append_q4_kernel<true> : kv_append_q4_kernel<false>;
+  if (pieces > kAppendQ4OneWG) {
+    q.counts = 0;
+    const int parts = (int)std::min<int64_t>(64, pieces / kAppendQ4PartPieces);
+    kernel<<<dim3(p.B, parts), dim3(kThreads), 0, stream>>>(q, lanes_log2(p.L));
+    const hipError_t e = hipGetLastError();
+    if (e != hipSuccess) return e;
+    q.copies = 0;
+    q.counts = 1;
+  }
+  kernel<<<dim3(p.B), dim3(kThreads), 0, stream>>>(q, lanes_log2(p.L));
   return hipGetLastError();
 }
 

@@ -356,7 +356,7 @@ def test_rows_that_are_not_asked_for_stay():
 
 
 @pytest.mark.parametrize("dtype", ["bf16", "f32"])
-@pytest.mark.parametrize("D,S,L", [(128, 8, 8), (64, 5, 3), (64, 1, 1), (128, 2, 300), (128, 1024, 1)])
+@pytest.mark.parametrize("D,S,L", [(128, 8, 8), (64, 5, 3), (64, 1, 1), (128, 2, 70), (128, 2, 300), (128, 1024, 1), (64, 64, 128)])
 def test_append(dtype, D, S, L):
     """The accepted tokens behind each row's prefix, as kv_append puts them there: lists
     that end early or name a slot twice, rows that do not fit."""
