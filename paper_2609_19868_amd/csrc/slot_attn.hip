@@ -147,6 +147,26 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
     vis_lo = p.cross ? 0 : own_lo;
   }
 
+  // ---- Q fragments (B operand of S^T = K Q^T), kept in registers; loaded
+  // and waited for before the direct-load pipeline starts so that the
+  // pipeline's counted waits see only its own loads
+  // (VIEW: requested before the tiles are worked out, waited for with the first)
+  bf16x8 qf[NKS];
+  auto load_q = [&]() __attribute__((always_inline)) {
+    const uint4* qrow = reinterpret_cast<const uint4*>(p.q + ((size_t)bg * p.R + (row_ok ? mrow : 0)) * D);
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {
+      uint4 v = row_ok ? qrow[2 * ks + hh] : make_uint4(0, 0, 0, 0);
+      qf[ks] = __builtin_bit_cast(bf16x8, v);
+    }
+  };
+  load_q();
+  if constexpr (VIEW == 0) {
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) lds_tie(qf[ks]);
+    wait_vmcnt<0>();
+  }
+
   // ---- key tiles of this workgroup: a range of prefix tiles, then (last
   // split only) the draft-token tiles covering every row's visible range.
   const int pre_begin = split * p.tiles_per_split;
@@ -187,26 +207,6 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
     tw1 = (min(p.R, rb * RB + wave_u * 32 + 32) - 1) / p.G;
   }
   auto is_pre = [&](int i) { return VIEW ? first + i < tiles.n_pre : i < n_pre; };
-
-  // ---- Q fragments (B operand of S^T = K Q^T), kept in registers; loaded
-  // and waited for before the direct-load pipeline starts so that the
-  // pipeline's counted waits see only its own loads
-  // (VIEW: after the first tile's loads, so that the two come together)
-  bf16x8 qf[NKS];
-  auto load_q = [&]() __attribute__((always_inline)) {
-    const uint4* qrow = reinterpret_cast<const uint4*>(p.q + ((size_t)bg * p.R + (row_ok ? mrow : 0)) * D);
-#pragma unroll
-    for (int ks = 0; ks < NKS; ++ks) {
-      uint4 v = row_ok ? qrow[2 * ks + hh] : make_uint4(0, 0, 0, 0);
-      qf[ks] = __builtin_bit_cast(bf16x8, v);
-    }
-  };
-  if constexpr (VIEW == 0) {
-    load_q();
-#pragma unroll
-    for (int ks = 0; ks < NKS; ++ks) lds_tie(qf[ks]);
-    wait_vmcnt<0>();
-  }
 
   // ---- direct-to-LDS staging of K and V tiles: load j of a wave fills 1 KB
   // chunk c = NWAVE*j + wave (RPC rows); lane l lands at row RPC*c + l/LPR,
@@ -514,6 +514,8 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
   // a wave of padding rows only helps to load the tiles (520 rows a group in
   // blocks of 128, Mode A: the step 211 -> 207 us)
   const bool live = rb * RB + wave_u * 32 < p.R;
+  constexpr std::integral_constant<int, 0> c0{};
+  constexpr std::integral_constant<int, 1> c1{};
   auto step = [&](int i, auto buf) __attribute__((always_inline)) {
     wait_vmcnt<0>();
     block_barrier();
@@ -530,11 +532,9 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
   };
   if constexpr (VIEW == 2) {
     if (nt > 0 && is_pre(0)) fetch_q4(0);
-    load_q();
     advance(0, 0);
   } else {
     if (nt > 0) issue(0, 0);
-    if constexpr (VIEW != 0) load_q();
   }
   if constexpr (VIEW != 0) {  // waited for here: in the loop it would be with every tile's loads
 #pragma unroll
@@ -542,8 +542,8 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
   }
   const int n_steps = GRP > 1 ? steps : nt;
   for (int i = 0; i < n_steps; i += 2) {
-    step(i, std::integral_constant<int, 0>{});
-    if (i + 1 < n_steps) step(i + 1, std::integral_constant<int, 1>{});
+    step(i, c0);
+    if (i + 1 < n_steps) step(i + 1, c1);
   }
 
   if constexpr (VIEW != 0) {
@@ -608,29 +608,87 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
     }
   }
 
-  if constexpr (GRP > 1) {
-    // the second group's sums to the first, lane by lane through the tile buffers
-    static_assert(GRP == 2 && NWAVE * (NDB * 16 + 2) * 64 * 4 <= (int)sizeof lds_all, "room for a group's sums");
-    float* x = reinterpret_cast<float*>(&lds_all[0][0][0][0]) + wave_u * (NDB * 16 + 2) * 64 + lane;
-    __syncthreads();
-    if (grp == 1) {
+  if constexpr (VIEW != 0) {
+    // ---- finalize.  Of two groups each takes half of the rows' elements and gets the
+    // other's sums of them, lane by lane through the tile buffers.
+    constexpr int DBG = NDB / GRP;  // 32-wide blocks taken
+    constexpr int XW = (DBG * 16 + 2) * 64;  // words that a wave is given
+    static_assert(GRP <= 2 && (GRP == 1 || GRP * NWAVE * XW * 4 <= (int)sizeof lds_all), "room for the sums");
+    const int d0 = grp * DBG * 32;
+    float* words = reinterpret_cast<float*>(&lds_all[0][0][0][0]);
+    f32x16 fin[DBG];
+    float m_fin = m_run, l_fin = l_run;
+    __syncthreads();  // every wave is done with the tiles
+    auto halves = [&](auto own) __attribute__((always_inline)) {
+      constexpr int MINE = decltype(own)::value * DBG, OTHER = NDB - DBG - MINE;
+      if constexpr (GRP > 1) {
+        float* to = words + ((grp ^ 1) * NWAVE + wave_u) * XW + lane;
+        const float* from = words + (grp * NWAVE + wave_u) * XW + lane;
 #pragma unroll
-      for (int db = 0; db < NDB; ++db)
+        for (int db = 0; db < DBG; ++db)
 #pragma unroll
-        for (int v = 0; v < 16; ++v) x[(db * 16 + v) * 64] = oacc[db][v];
-      x[NDB * 16 * 64] = m_run;
-      x[(NDB * 16 + 1) * 64] = l_run;
+          for (int v = 0; v < 16; ++v) to[(db * 16 + v) * 64] = oacc[OTHER + db][v];
+        to[DBG * 16 * 64] = m_run;
+        to[(DBG * 16 + 1) * 64] = l_run;
+        __syncthreads();
+        const float m1 = from[DBG * 16 * 64], l1 = from[(DBG * 16 + 1) * 64];
+        m_fin = fmaxf(m_run, m1);
+        const float a0 = fast_exp2((m_run - m_fin) * c2), a1 = fast_exp2((m1 - m_fin) * c2);
+        l_fin = l_run * a0 + l1 * a1;
+#pragma unroll
+        for (int db = 0; db < DBG; ++db)
+#pragma unroll
+          for (int v = 0; v < 16; ++v) fin[db][v] = oacc[MINE + db][v] * a0 + from[(db * 16 + v) * 64] * a1;
+      } else {
+#pragma unroll
+        for (int db = 0; db < DBG; ++db) fin[db] = oacc[db];
+      }
+    };
+    if (grp == 0) {
+      halves(c0);
+    } else if constexpr (GRP > 1) {
+      halves(c1);
     }
-    __syncthreads();
-    if (grp == 1) return;
-    const float m1 = x[NDB * 16 * 64], m_new = fmaxf(m_run, m1);
-    const float a0 = fast_exp2((m_run - m_new) * c2), a1 = fast_exp2((m1 - m_new) * c2);
-    l_run = l_run * a0 + x[(NDB * 16 + 1) * 64] * a1;
-    m_run = m_new;
+    const float l_tot = sum_xor32(l_fin);
+    const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+    const float lse2 = m_fin * c2 + __log2f(l_tot);  // log2 units
+    const size_t grow0 = (size_t)bg * p.R;
+    if (p.n_split == 1) {
+      // rows of the output by 16 neighbouring bytes a lane, turned in an LDS piece of the
+      // wave's own (training layout under a window of 1024, with the queries requested
+      // first: 326 -> 308 us; 1.7B verification over 4-bit keys 29.9 -> 27.6)
+      constexpr int CH = DBG * 4;  // 16-byte pieces of a row
+      uint8_t* own = reinterpret_cast<uint8_t*>(words) + (grp * NWAVE + wave_u) * (GRP > 1 ? XW * 4 : 32 * CH * 16);
 #pragma unroll
-    for (int db = 0; db < NDB; ++db)
+      for (int db = 0; db < DBG; ++db)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) oacc[db][v] = oacc[db][v] * a0 + x[(db * 16 + v) * 64] * a1;
+        for (int u = 0; u < 4; ++u) {
+          uint2 pk;
+          pk.x = pack_bf16x2_hw(fin[db][4 * u] * inv, fin[db][4 * u + 1] * inv);
+          pk.y = pack_bf16x2_hw(fin[db][4 * u + 2] * inv, fin[db][4 * u + 3] * inv);
+          *reinterpret_cast<uint2*>(own + n * (CH * 16) + (((db * 4 + u) ^ (n & (CH - 1))) << 4) + hh * 8) = pk;
+        }
+      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's writes before its reads
+#pragma unroll
+      for (int i = 0; i < CH / 2; ++i) {
+        const int r = i * (64 / CH) + lane / CH, c = lane % CH;
+        const uint4 v = *reinterpret_cast<const uint4*>(own + r * (CH * 16) + ((c ^ (r & (CH - 1))) << 4));
+        const int at = __shfl(row_ok ? mrow : -1, r);
+        if (at >= 0) *reinterpret_cast<uint4*>(p.out + (grow0 + at) * D + d0 + 8 * c) = v;
+      }
+      if (p.lse && hh == 0 && grp == 0 && row_ok) p.lse[grow0 + mrow] = lse2 * kLn2;
+    } else if (row_ok) {
+      const size_t prow = (size_t)split * p.rows_total + grow0 + mrow;
+#pragma unroll
+      for (int db = 0; db < DBG; ++db)
+#pragma unroll
+        for (int u = 0; u < 4; ++u)
+          *reinterpret_cast<float4*>(p.part_o + prow * D + d0 + db * 32 + 8 * u + 4 * hh) =
+              make_float4(fin[db][4 * u] * inv, fin[db][4 * u + 1] * inv, fin[db][4 * u + 2] * inv,
+                          fin[db][4 * u + 3] * inv);
+      if (hh == 0 && grp == 0) p.part_lse[prow] = l_tot > 0.f ? lse2 : -INFINITY;
+    }
+    return;
   }
 
   // ---- finalize: combine the two lane halves' partial sums
@@ -642,7 +700,7 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
     // the same, instead of kept in a register through the loop
     int te = tid;
     asm volatile("" : "+v"(te));
-    const int row_e = rb * RB + (GRP > 1 ? (te >> 6) % NWAVE : te >> 6) * 32 + (te & 31);
+    const int row_e = rb * RB + (te >> 6) * 32 + (te & 31);
     orow_in = (row_e % p.G) * p.T + row_e / p.G;
   }
   const size_t grow = (size_t)bg * p.R + orow_in;  // row of the [B*Hq*T] output
