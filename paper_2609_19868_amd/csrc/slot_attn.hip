@@ -30,7 +30,6 @@
 #include <type_traits>
 #include <utility>
 
-#include "attn_view.hpp"
 #include "common.hpp"
 #include "kernels.hpp"
 
@@ -78,11 +77,9 @@ __host__ __device__ constexpr int swz(int kr) {
 // the kernel keeps to 128 registers, which short prefixes of many sequences need
 // (71 x 8 groups of 153 rows, 470 keys: 43.4 us, and 54.6 with the 154 registers
 // and three waves that the compiler takes when it is left to).
-//
-// VIEW: 0 the whole prefix, 1 a window of it, 2 a cache of 4-bit codes (with or
-// without a window); see slot_view_bf16_kernel below.
-template <int D, int NWAVE, int VIEW, int GRP, class Params>
-__device__ __forceinline__ void attn_bf16_body(const Params& p) {
+template <int D, int NWAVE>
+__global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : ZARYA_ATTN_WPE))) void slot_attn_bf16_kernel(
+    AttnParams p) {
   constexpr int RB = NWAVE * 32;        // query rows per workgroup
   constexpr int ROWB = D * 2;           // bytes per key row
   constexpr int TILEB = KT * ROWB;      // bytes of one K (or V) tile
@@ -92,7 +89,7 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
   constexpr int NDB = D / 32;           // 32-wide blocks of the head dim
   constexpr int NKS = D / 16;           // k-steps of the QK^T contraction
   static_assert(CPW * NWAVE * 1024 == TILEB, "tile must split into 1 KB chunks per wave");
-  __shared__ __attribute__((aligned(16))) uint8_t lds_all[GRP][2][2][TILEB];
+  __shared__ __attribute__((aligned(16))) uint8_t lds[2][2][TILEB];
 
   int rb, split, bg;  // row block, prefix split, b * Hkv + g
   if (p.heavy_first) {
@@ -106,9 +103,8 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
     split = 0;
     bg = x * gpx + k % gpx;
   } else {
-    int w = xcd_work_index(blockIdx.x, p.per_xcd, p.n_items);
+    const int w = xcd_work_index(blockIdx.x, p.per_xcd, p.n_items);
     if (w < 0) return;
-    if constexpr (VIEW != 0) w += p.item0;
     rb = w % p.n_rb;
     split = (w / p.n_rb) % p.n_split;
     bg = w / (p.n_rb * p.n_split);
@@ -119,12 +115,7 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
 
   const int tid = threadIdx.x;
   const int lane = tid & 63, wave = tid >> 6;
-  const int wave_all = __builtin_amdgcn_readfirstlane(wave);
-  // GRP > 1: groups of NWAVE waves hold the same rows and take a share of the
-  // tiles each, with LDS buffers of their own
-  const int grp = GRP > 1 ? wave_all / NWAVE : 0;
-  const int wave_u = GRP > 1 ? wave_all % NWAVE : wave_all;
-  auto& lds = lds_all[grp];
+  const int wave_u = __builtin_amdgcn_readfirstlane(wave);
   const int n = lane & 31, hh = lane >> 5;
 
   // ---- this lane's query row and its visible range [vis_lo, vis_hi) of
@@ -132,39 +123,17 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
   // h), so a block's rows cover a contiguous token range of every head of
   // the group and share one visible key range; mrow is the row's place in
   // the head-major [G, T] layout of q and out.
-  const int row = rb * RB + (GRP > 1 ? wave_u : wave) * 32 + n;
+  const int row = rb * RB + wave * 32 + n;
   const bool row_ok = row < p.R;
   const int mrow = (row % p.G) * p.T + row / p.G;
   int vis_lo = 0, vis_hi = 0;
-  int win_lo = 0;  // VIEW: the first draft key inside the row's window
   if (row_ok) {
     const int t = row / p.G;
-    if constexpr (VIEW != 0) win_lo = t - p.window + 1;
     const int s = t / p.L, r = t - s * p.L;
     const int pass = p.slot_pass ? (int)p.slot_pass[b * p.S + s] : p.pass;
     const int own_lo = s * p.L;
     vis_hi = own_lo + (pass == 0 ? p.L : r + 1);
     vis_lo = p.cross ? 0 : own_lo;
-  }
-
-  // ---- Q fragments (B operand of S^T = K Q^T), kept in registers; loaded
-  // and waited for before the direct-load pipeline starts so that the
-  // pipeline's counted waits see only its own loads
-  // (VIEW: requested before the tiles are worked out, waited for with the first)
-  bf16x8 qf[NKS];
-  auto load_q = [&]() __attribute__((always_inline)) {
-    const uint4* qrow = reinterpret_cast<const uint4*>(p.q + ((size_t)bg * p.R + (row_ok ? mrow : 0)) * D);
-#pragma unroll
-    for (int ks = 0; ks < NKS; ++ks) {
-      uint4 v = row_ok ? qrow[2 * ks + hh] : make_uint4(0, 0, 0, 0);
-      qf[ks] = __builtin_bit_cast(bf16x8, v);
-    }
-  };
-  load_q();
-  if constexpr (VIEW == 0) {
-#pragma unroll
-    for (int ks = 0; ks < NKS; ++ks) lds_tie(qf[ks]);
-    wait_vmcnt<0>();
   }
 
   // ---- key tiles of this workgroup: a range of prefix tiles, then (last
@@ -181,32 +150,23 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
     slot_lo = (lo / KT) * KT;
     n_slot = (hi - slot_lo + KT - 1) / KT;
   }
-  int nt = n_pre + n_slot;
-  // VIEW: the listed tiles of the block's tokens are shared out among the splits
-  // by their number in this batch row, tile i of this workgroup being the list's
-  // first + i; tokens tw0..tw1 are this wave's
-  KeyTiles<KT> tiles;
-  int first = 0, tw0 = 0, tw1 = 0;
-  int steps = 0;  // VIEW: tiles of the group that has the most
-  if constexpr (VIEW != 0) {
-    const int t0 = rb * RB / p.G, t1 = (min(p.R, rb * RB + RB) - 1) / p.G;
-    tiles.list(Pb, t0, p.cross ? 0 : t0 / p.L * p.L,
-               p.pass != 0 && !p.slot_pass ? t1 + 1 : min(p.T, (t1 / p.L + 1) * p.L), p.window, p.sinks);
-    const int per_split = (tiles.nt + p.n_split - 1) / p.n_split;
-    first = min(split * per_split, tiles.nt);
-    nt = min(per_split, tiles.nt - first);
-    if constexpr (GRP > 1) {
-      steps = (nt + GRP - 1) / GRP;
-      const int skip = min(grp * steps, nt);
-      first += skip;
-      nt = min(steps, nt - skip);
-    } else {
-      steps = nt;
+  const int nt = n_pre + n_slot;
+
+  // ---- Q fragments (B operand of S^T = K Q^T), kept in registers; loaded
+  // and waited for before the direct-load pipeline starts so that the
+  // pipeline's counted waits see only its own loads
+  bf16x8 qf[NKS];
+  {
+    const uint4* qrow = reinterpret_cast<const uint4*>(p.q + ((size_t)bg * p.R + (row_ok ? mrow : 0)) * D);
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {
+      uint4 v = row_ok ? qrow[2 * ks + hh] : make_uint4(0, 0, 0, 0);
+      qf[ks] = __builtin_bit_cast(bf16x8, v);
     }
-    tw0 = (rb * RB + wave_u * 32) / p.G;
-    tw1 = (min(p.R, rb * RB + wave_u * 32 + 32) - 1) / p.G;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) lds_tie(qf[ks]);
+    wait_vmcnt<0>();
   }
-  auto is_pre = [&](int i) { return VIEW ? first + i < tiles.n_pre : i < n_pre; };
 
   // ---- direct-to-LDS staging of K and V tiles: load j of a wave fills 1 KB
   // chunk c = NWAVE*j + wave (RPC rows); lane l lands at row RPC*c + l/LPR,
@@ -227,13 +187,7 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
   auto issue = [&](int i, int buf) __attribute__((always_inline)) {
     const char *kp, *vp;
     int key0, valid;
-    if constexpr (VIEW != 0) {
-      const bool pre = VIEW == 1 && is_pre(i);
-      key0 = tiles.key0(first + i);
-      kp = pre ? kc : ks_;
-      vp = pre ? vc : vs_;
-      valid = (pre ? Pb : p.T) - key0;
-    } else if (i < n_pre) {
+    if (i < n_pre) {
       key0 = (pre_begin + i) * KT;
       kp = kc;
       vp = vc;
@@ -262,62 +216,6 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
         dma16(vp + my_off[j] + dr * ROWB, vd + NWAVE * j * 1024);
       }
     }
-  };
-
-  // ---- 4-bit tiles: a block of 32 codes (16 bytes) and its scale byte per
-  // thread and piece, requested two tiles ahead into registers and converted into
-  // the tile's bf16 image in LDS one tile ahead
-  constexpr int NB = D / 32;                             // blocks per row
-  constexpr int NPC = 2 * KT * NB;                       // K's pieces, then V's
-  constexpr int PCS = (NPC + NWAVE * 64 - 1) / (NWAVE * 64);  // per thread
-  uint4 codes[PCS];
-  uint32_t scales[PCS];
-  auto piece = [&](int j, int& which, int& r, int& blk) __attribute__((always_inline)) {
-    const int c0 = wave_u * 64 + j * NWAVE * 64;  // wave-uniform; KT * NB is a multiple of 64
-    which = c0 / (KT * NB);
-    const int c = c0 % (KT * NB) + lane;
-    r = c / NB;
-    blk = c % NB;
-    return c0 < NPC;
-  };
-  auto fetch_q4 = [&](int i) __attribute__((always_inline)) {
-    if constexpr (VIEW == 2) {
-      const int key0 = tiles.key0(first + i);
-      const size_t base = (size_t)bg * p.C + key0;
-#pragma unroll
-      for (int j = 0; j < PCS; ++j) {
-        int which, r, blk;
-        if (!piece(j, which, r, blk)) continue;
-        r = min(r, Pb - key0 - 1);  // rows past the valid keys follow the last one
-        const uint8_t* cp = reinterpret_cast<const uint8_t*>(which ? p.v_cache : p.k_cache) + base * (D / 2);
-        const uint8_t* sp = (which ? p.v_scale : p.k_scale) + base * NB;
-        codes[j] = *reinterpret_cast<const uint4*>(cp + (uint32_t)(r * (D / 2) + blk * 16));
-        scales[j] = sp[(uint32_t)(r * NB + blk)];
-      }
-    }
-  };
-  auto unpack_q4 = [&](int buf) __attribute__((always_inline)) {
-#pragma unroll
-    for (int j = 0; j < PCS; ++j) {
-      int which, r, blk;
-      if (!piece(j, which, r, blk)) continue;
-      uint8_t* dst = &lds[buf][which][r * ROWB];
-      const float sc = q4_scale(scales[j]);
-      const uint32_t cw[4] = {codes[j].x, codes[j].y, codes[j].z, codes[j].w};
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        *reinterpret_cast<bf16x8*>(dst + (((4 * blk + e) ^ swz<D>(r)) << 4)) = q4_bf16x8(cw[e], sc);
-    }
-  };
-  // tile j into buffer buf: its codes are in registers, or it is loaded directly
-  auto advance = [&](int j, int buf) __attribute__((always_inline)) {
-    if (j >= nt) return;
-    if (is_pre(j)) {
-      unpack_q4(buf);
-    } else {
-      issue(j, buf);
-    }
-    if (j + 1 < nt && is_pre(j + 1)) fetch_q4(j + 1);
   };
 
   f32x16 oacc[NDB];
@@ -395,30 +293,12 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
 
   // ---- online softmax of tile i's scores; masks only on tiles that need them
   auto softmax = [&](int i) __attribute__((always_inline)) {
-    const bool is_slot = !is_pre(i);
-    const int key0 = VIEW ? tiles.key0(first + i) : is_slot ? slot_lo + (i - n_pre) * KT : (pre_begin + i) * KT;
+    const bool is_slot = i >= n_pre;
+    const int key0 = is_slot ? slot_lo + (i - n_pre) * KT : (pre_begin + i) * KT;
     const bool full = !is_slot && key0 + KT <= Pb;
     const int lim_lo = is_slot ? vis_lo : key0;
     const int lim_n = is_slot ? vis_hi - vis_lo : Pb - key0;
-    if constexpr (VIEW != 0) {
-      // nothing to hide: every key shown to every token of the wave by the pass,
-      // and all of them sinks or inside the last token's window
-      const int off = is_slot ? 0 : Pb;  // places of the tile's keys less their indices, as seen from the tokens
-      const int sink_hi = is_slot ? p.sinks - Pb : p.sinks;
-      const bool shown = is_slot ? key0 >= (p.cross ? 0 : tw1 / p.L * p.L) && key0 + KT <= tw0 + 1 : key0 + KT <= Pb;
-      const bool masked = !(shown && (key0 + KT <= sink_hi || key0 > off + tw1 - p.window));
-      if (masked) {
-        // the row's keys as bits: below(x), the tile's keys under x
-        auto below = [&](int x) { return x <= key0 ? 0ull : x - key0 >= KT ? ~0ull : (1ull << (x - key0)) - 1; };
-        const uint64_t m = below(lim_lo + lim_n) & ~below(lim_lo) & (below(sink_hi) | ~below(win_lo + off));
-        const uint32_t seen[2] = {(uint32_t)m >> (4 * hh), (uint32_t)(m >> 32) >> (4 * hh)};
-#pragma unroll
-        for (int kb = 0; kb < 2; ++kb)
-#pragma unroll
-          for (int v = 0; v < 16; ++v)
-            if (!(seen[kb] >> (8 * (v >> 2) + (v & 3)) & 1)) sacc[kb][v] = -INFINITY;
-      }
-    } else if (!full) {
+    if (!full) {
 #pragma unroll
       for (int kb = 0; kb < 2; ++kb)
 #pragma unroll
@@ -514,181 +394,20 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
   // a wave of padding rows only helps to load the tiles (520 rows a group in
   // blocks of 128, Mode A: the step 211 -> 207 us)
   const bool live = rb * RB + wave_u * 32 < p.R;
-  constexpr std::integral_constant<int, 0> c0{};
-  constexpr std::integral_constant<int, 1> c1{};
   auto step = [&](int i, auto buf) __attribute__((always_inline)) {
     wait_vmcnt<0>();
     block_barrier();
-    if constexpr (VIEW == 2) {
-      advance(i + 1, decltype(buf)::value ^ 1);
-    } else {
-      if (i + 1 < nt) issue(i + 1, decltype(buf)::value ^ 1);
-    }
-    if (!live || (GRP > 1 && i >= nt)) return;
+    if (i + 1 < nt) issue(i + 1, decltype(buf)::value ^ 1);
+    if (!live) return;
     qk(buf);
     pv_read(buf, std::integral_constant<int, 0>{});  // in flight during the softmax
     softmax(i);
     pv(buf);
   };
-  if constexpr (VIEW == 2) {
-    if (nt > 0 && is_pre(0)) fetch_q4(0);
-    advance(0, 0);
-  } else {
-    if (nt > 0) issue(0, 0);
-  }
-  if constexpr (VIEW != 0) {  // waited for here: in the loop it would be with every tile's loads
-#pragma unroll
-    for (int ks = 0; ks < NKS; ++ks) lds_tie(qf[ks]);
-  }
-  const int n_steps = GRP > 1 ? steps : nt;
-  for (int i = 0; i < n_steps; i += 2) {
-    step(i, c0);
-    if (i + 1 < n_steps) step(i + 1, c1);
-  }
-
-  if constexpr (VIEW != 0) {
-    // A value that is not finite has left its mark on the sums of every row whose
-    // tile held it, seen or not (0 * inf).  Then the wave's sums are taken once
-    // more, key by key over the visible ones (the maxima and the sums of the
-    // probabilities never saw the others).
-    float z = 0.f;
-#pragma unroll
-    for (int db = 0; db < NDB; ++db)
-#pragma unroll
-      for (int v = 0; v < 16; ++v) z = fmaf(oacc[db][v], 0.f, z);
-    if (__any(row_ok && z != 0.f)) {
-#pragma unroll
-      for (int db = 0; db < NDB; ++db) oacc[db] = f32x16{};
-      // eight elements from d on of a row of K (which = 0) or V
-      auto row8 = [&](bool pre, int which, int key, int d) __attribute__((always_inline)) {
-        if (VIEW == 2 && pre) {
-          const size_t at = (size_t)bg * p.C + key;
-          const uint8_t* cp = reinterpret_cast<const uint8_t*>(which ? p.v_cache : p.k_cache) + at * (D / 2) + d / 2;
-          return q4_bf16x8(*reinterpret_cast<const uint32_t*>(cp),
-                           q4_scale((which ? p.v_scale : p.k_scale)[at * NB + d / 32]));
-        }
-        const char* base = pre ? (which ? vc : kc) : which ? vs_ : ks_;
-        return *reinterpret_cast<const bf16x8*>(base + (size_t)key * ROWB + d * 2);
-      };
-      const uint16_t* qrow = p.q + ((size_t)bg * p.R + (row_ok ? mrow : 0)) * D;
-#pragma unroll 1
-      for (int i = 0; i < nt; ++i) {
-        const bool pre = is_pre(i);
-        const int key0 = tiles.key0(first + i), end = min(key0 + KT, pre ? Pb : p.T);
-        const int off = pre ? Pb : 0;
-#pragma unroll 1
-        for (int key = key0; key < end; ++key) {
-          const bool ok = row_ok && (pre || (key >= vis_lo && key < vis_hi)) &&
-                          (key < p.sinks - (pre ? 0 : Pb) || key >= win_lo + off);
-          if (!__any(ok)) continue;
-          float sc = 0.f;
-#pragma unroll 1
-          for (int c = 0; c < D / 2; c += 8) {
-            const int d = hh * (D / 2) + c;
-            const bf16x8 qv = *reinterpret_cast<const bf16x8*>(qrow + d), kv = row8(pre, 0, key, d);
-#pragma unroll
-            for (int e = 0; e < 8; ++e) sc = fmaf((float)qv[e], (float)kv[e], sc);
-          }
-          sc = sum_xor32(sc);
-          const float pr = (float)(__bf16)fast_exp2(fmaf(sc, c2, -(m_run * c2)));
-#pragma unroll
-          for (int db = 0; db < NDB; ++db)
-#pragma unroll
-            for (int u = 0; u < 4; ++u) {
-              const bf16x8 vv = row8(pre, 1, key, db * 32 + 8 * u);
-#pragma unroll
-              for (int e = 0; e < 4; ++e) {
-                const float x = hh ? (float)vv[4 + e] : (float)vv[e];
-                oacc[db][4 * u + e] = ok ? fmaf(pr, x, oacc[db][4 * u + e]) : oacc[db][4 * u + e];
-              }
-              __builtin_amdgcn_sched_barrier(0);  // one piece at a time: no more registers than the loop above
-            }
-        }
-      }
-    }
-  }
-
-  if constexpr (VIEW != 0) {
-    // ---- finalize.  Of two groups each takes half of the rows' elements and gets the
-    // other's sums of them, lane by lane through the tile buffers.
-    constexpr int DBG = NDB / GRP;  // 32-wide blocks taken
-    constexpr int XW = (DBG * 16 + 2) * 64;  // words that a wave is given
-    static_assert(GRP <= 2 && (GRP == 1 || GRP * NWAVE * XW * 4 <= (int)sizeof lds_all), "room for the sums");
-    const int d0 = grp * DBG * 32;
-    float* words = reinterpret_cast<float*>(&lds_all[0][0][0][0]);
-    f32x16 fin[DBG];
-    float m_fin = m_run, l_fin = l_run;
-    __syncthreads();  // every wave is done with the tiles
-    auto halves = [&](auto own) __attribute__((always_inline)) {
-      constexpr int MINE = decltype(own)::value * DBG, OTHER = NDB - DBG - MINE;
-      if constexpr (GRP > 1) {
-        float* to = words + ((grp ^ 1) * NWAVE + wave_u) * XW + lane;
-        const float* from = words + (grp * NWAVE + wave_u) * XW + lane;
-#pragma unroll
-        for (int db = 0; db < DBG; ++db)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) to[(db * 16 + v) * 64] = oacc[OTHER + db][v];
-        to[DBG * 16 * 64] = m_run;
-        to[(DBG * 16 + 1) * 64] = l_run;
-        __syncthreads();
-        const float m1 = from[DBG * 16 * 64], l1 = from[(DBG * 16 + 1) * 64];
-        m_fin = fmaxf(m_run, m1);
-        const float a0 = fast_exp2((m_run - m_fin) * c2), a1 = fast_exp2((m1 - m_fin) * c2);
-        l_fin = l_run * a0 + l1 * a1;
-#pragma unroll
-        for (int db = 0; db < DBG; ++db)
-#pragma unroll
-          for (int v = 0; v < 16; ++v) fin[db][v] = oacc[MINE + db][v] * a0 + from[(db * 16 + v) * 64] * a1;
-      } else {
-#pragma unroll
-        for (int db = 0; db < DBG; ++db) fin[db] = oacc[db];
-      }
-    };
-    if (grp == 0) {
-      halves(c0);
-    } else if constexpr (GRP > 1) {
-      halves(c1);
-    }
-    const float l_tot = sum_xor32(l_fin);
-    const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
-    const float lse2 = m_fin * c2 + __log2f(l_tot);  // log2 units
-    const size_t grow0 = (size_t)bg * p.R;
-    if (p.n_split == 1) {
-      // rows of the output by 16 neighbouring bytes a lane, turned in an LDS piece of the
-      // wave's own (training layout under a window of 1024, with the queries requested
-      // first: 326 -> 308 us; 1.7B verification over 4-bit keys 29.9 -> 27.6)
-      constexpr int CH = DBG * 4;  // 16-byte pieces of a row
-      uint8_t* own = reinterpret_cast<uint8_t*>(words) + (grp * NWAVE + wave_u) * (GRP > 1 ? XW * 4 : 32 * CH * 16);
-#pragma unroll
-      for (int db = 0; db < DBG; ++db)
-#pragma unroll
-        for (int u = 0; u < 4; ++u) {
-          uint2 pk;
-          pk.x = pack_bf16x2_hw(fin[db][4 * u] * inv, fin[db][4 * u + 1] * inv);
-          pk.y = pack_bf16x2_hw(fin[db][4 * u + 2] * inv, fin[db][4 * u + 3] * inv);
-          *reinterpret_cast<uint2*>(own + n * (CH * 16) + (((db * 4 + u) ^ (n & (CH - 1))) << 4) + hh * 8) = pk;
-        }
-      asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's writes before its reads
-#pragma unroll
-      for (int i = 0; i < CH / 2; ++i) {
-        const int r = i * (64 / CH) + lane / CH, c = lane % CH;
-        const uint4 v = *reinterpret_cast<const uint4*>(own + r * (CH * 16) + ((c ^ (r & (CH - 1))) << 4));
-        const int at = __shfl(row_ok ? mrow : -1, r);
-        if (at >= 0) *reinterpret_cast<uint4*>(p.out + (grow0 + at) * D + d0 + 8 * c) = v;
-      }
-      if (p.lse && hh == 0 && grp == 0 && row_ok) p.lse[grow0 + mrow] = lse2 * kLn2;
-    } else if (row_ok) {
-      const size_t prow = (size_t)split * p.rows_total + grow0 + mrow;
-#pragma unroll
-      for (int db = 0; db < DBG; ++db)
-#pragma unroll
-        for (int u = 0; u < 4; ++u)
-          *reinterpret_cast<float4*>(p.part_o + prow * D + d0 + db * 32 + 8 * u + 4 * hh) =
-              make_float4(fin[db][4 * u] * inv, fin[db][4 * u + 1] * inv, fin[db][4 * u + 2] * inv,
-                          fin[db][4 * u + 3] * inv);
-      if (hh == 0 && grp == 0) p.part_lse[prow] = l_tot > 0.f ? lse2 : -INFINITY;
-    }
-    return;
+  if (nt > 0) issue(0, 0);
+  for (int i = 0; i < nt; i += 2) {
+    step(i, std::integral_constant<int, 0>{});
+    if (i + 1 < nt) step(i + 1, std::integral_constant<int, 1>{});
   }
 
   // ---- finalize: combine the two lane halves' partial sums
@@ -732,19 +451,6 @@ __device__ __forceinline__ void attn_bf16_body(const Params& p) {
       }
     if (hh == 0) p.part_lse[(size_t)split * p.rows_total + grow] = l_tot > 0.f ? lse2 : -INFINITY;
   }
-}
-
-template <int D, int NWAVE>
-__global__ __launch_bounds__(NWAVE * 64) __attribute__((amdgpu_waves_per_eu(D == 64 ? 4 : ZARYA_ATTN_WPE))) void slot_attn_bf16_kernel(
-    AttnParams p) {
-  attn_bf16_body<D, NWAVE, 0, 1, AttnParams>(p);
-}
-
-// The same kernel over a bounded view of the prefix.
-template <int D, int NWAVE, int VIEW, int GRP>
-__global__ __launch_bounds__(NWAVE * GRP * 64) __attribute__((amdgpu_waves_per_eu(2))) void slot_view_bf16_kernel(
-    ViewParams p) {
-  attn_bf16_body<D, NWAVE, VIEW, GRP, ViewParams>(p);
 }
 
 // Exact merge of the prefix splits: O = sum_i w_i O_i / sum_i w_i with
@@ -853,11 +559,8 @@ __global__ __launch_bounds__(256) void slot_attn_merge_kernel(const float* __res
 // workgroup's barriers and LDS, one or two workgroups a unit, for a tile each.
 // 4096 groups, D = 128: 1 row x 1 key 112 us with eight waves, 18 with one; 4 rows
 // x 68 keys 165 and 70; 4 rows x 516 keys 529 and 387.
-//
-// VIEW as in attn_bf16_body.  With 4-bit codes the contraction is taken in another
-// order, in which a lane's elements of a key are one run: a quarter of the row.
-template <int D, int NR, int DS, int NW, int VIEW, class Params>
-__device__ __forceinline__ void attn_f32_body(const Params& p) {
+template <int D, int NR, int DS, int NW>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void slot_attn_f32_kernel(AttnParams32 p) {
   constexpr int RB = 16 * NR;   // query rows per workgroup
   constexpr int NKS = D / 16;   // 16-byte pieces of a K row per lane
   constexpr int DO = D / DS;    // elements of the output row taken by this workgroup
@@ -865,8 +568,6 @@ __device__ __forceinline__ void attn_f32_body(const Params& p) {
   constexpr int NOB = DO / 16;  // 16-wide blocks of the output: block 4 * c + e holds d = 64 * c + 4 * i + e
   constexpr int OSTR = DO + 4;  // row stride of the partial outputs in LDS
   constexpr int QSTR = D + 4;   // and of the queries
-  constexpr int KQ = VIEW == 2 ? D / 4 : 4;   // element of a lane's first K piece, per lane quarter
-  constexpr int KP = VIEW == 2 ? 4 : 16;      // from one piece to the next
   __shared__ __attribute__((aligned(16))) float part_o[NW][RB][OSTR];
   __shared__ __attribute__((aligned(16))) float qs[RB][QSTR];  // scaled queries; the padding spreads the rows over the banks
   __shared__ float part_m[NW][RB], part_l[NW][RB];
@@ -886,12 +587,10 @@ __device__ __forceinline__ void attn_f32_body(const Params& p) {
   // this lane's query rows (one per row tile) and their visible draft keys;
   // rows past the end follow the last one and are not stored
   int vis_lo[NR], vis_hi[NR];
-  int win_lo[NR];  // VIEW: the first draft key inside the row's window
 #pragma unroll
   for (int r = 0; r < NR; ++r) {
     const int row = min(rb * RB + 16 * r + n, R - 1);
     const int t = row / p.G, s = t / p.L;
-    if constexpr (VIEW != 0) win_lo[r] = t - p.window + 1;
     const int pass = p.slot_pass ? (int)p.slot_pass[b * p.S + s] : p.pass;
     vis_hi[r] = pass == 0 ? (s + 1) * p.L : t + 1;
     vis_lo[r] = p.cross ? 0 : s * p.L;
@@ -903,24 +602,13 @@ __device__ __forceinline__ void attn_f32_body(const Params& p) {
     *reinterpret_cast<f32x4*>(&qs[lr][c]) = load_f32x4(p.q + qr * D + c) * p.scale;
   }
   __syncthreads();
-  const uint32_t q_addr = lds_addr(&qs[n][KQ * q4]);
+  const uint32_t q_addr = lds_addr(&qs[n][4 * q4]);
 
   // key tiles: the prefix's, then those covering the block's draft keys
-  int n_pre = (Pb + 15) / 16;
+  const int n_pre = (Pb + 15) / 16;
   const int t0 = rb * RB / p.G, t1 = (min(R, rb * RB + RB) - 1) / p.G;
   const int slot_lo = (p.cross ? 0 : (t0 / p.L) * p.L) & ~15;
-  int nt = n_pre + (min(p.T, (t1 / p.L + 1) * p.L) - slot_lo + 15) / 16;
-  KeyTiles<16> tiles;
-  if constexpr (VIEW != 0) {
-    tiles.list(Pb, t0, p.cross ? 0 : t0 / p.L * p.L,
-               p.pass != 0 && !p.slot_pass ? t1 + 1 : min(p.T, (t1 / p.L + 1) * p.L), p.window, p.sinks);
-    n_pre = tiles.n_pre;
-    nt = tiles.nt;
-  }
-  auto key0_of = [&](int i) __attribute__((always_inline)) {
-    if constexpr (VIEW != 0) return tiles.key0(i);
-    return i < n_pre ? 16 * i : slot_lo + 16 * (i - n_pre);
-  };
+  const int nt = n_pre + (min(p.T, (t1 / p.L + 1) * p.L) - slot_lo + 15) / 16;
   const float* kc = p.k_cache + (size_t)bg * p.C * D;
   const float* vc = p.v_cache + (size_t)bg * p.C * D + d0;
   const float* ks_ = p.k_slot + (size_t)bg * p.T * D;
@@ -937,43 +625,19 @@ __device__ __forceinline__ void attn_f32_body(const Params& p) {
   }
 
   f32x4 kf[NKS];
-  uint32_t kcode[NKS / 2], kscale = 0;  // VIEW 2: a prefix tile's codes, two pieces a word, and their scale
   // K row n of tile i, clamped to the last valid key (its score is masked)
   auto load_k = [&](int i) {
     const bool pre = i < n_pre;
-    const int key0 = key0_of(i);
-    const int key = min(key0 + n, (pre ? Pb : p.T) - 1);
-    if constexpr (VIEW == 2) {
-      if (pre) {
-        const size_t at = (size_t)bg * p.C + key;
-        const uint32_t* src = reinterpret_cast<const uint32_t*>(p.k_cache) + at * (D / 8) + q4 * (D / 32);
+    const int key0 = pre ? 16 * i : slot_lo + 16 * (i - n_pre);
+    const float* src = (pre ? kc : ks_) + (size_t)min(key0 + n, (pre ? Pb : p.T) - 1) * D + 4 * q4;
 #pragma unroll
-        for (int e = 0; e < NKS / 2; ++e) kcode[e] = src[e];
-        kscale = p.k_scale[at * (D / 32) + q4 * (D / 4) / 32];
-        return;
-      }
-    }
-    const float* src = (pre ? kc : ks_) + (size_t)key * D + KQ * q4;
-#pragma unroll
-    for (int ks = 0; ks < NKS; ++ks) kf[ks] = load_f32x4(src + KP * ks);
-  };
-  // four elements of V row `key` from d on (d0: the first taken by this workgroup);
-  // `row`: the same row of a cache that is not in 4 bits
-  auto load_v4 = [&](bool pre, int key, int d, const float* row) __attribute__((always_inline)) {
-    if constexpr (VIEW == 2) {
-      if (pre) {
-        const size_t at = (size_t)bg * p.C + key;
-        const uint32_t c = reinterpret_cast<const uint16_t*>(p.v_cache)[at * (D / 4) + (d0 + d) / 4];
-        return q4_f32x4(c, q4_scale(p.v_scale[at * (D / 32) + (d0 + d) / 32]));
-      }
-    }
-    return load_f32x4(row + d);
+    for (int ks = 0; ks < NKS; ++ks) kf[ks] = load_f32x4(src + 16 * ks);
   };
 
   if (wave < nt) load_k(wave);
   for (int i = wave; i < nt; i += NW) {
     const bool pre = i < n_pre;
-    const int key0 = key0_of(i);
+    const int key0 = pre ? 16 * i : slot_lo + 16 * (i - n_pre);
     const int last = (pre ? Pb : p.T) - 1;
     const float* vsrc = pre ? vc : vs_;
     f32x4 vf[4][NC];  // V rows 4 * q4 + v, elements 64 * c + 4 * n + e
@@ -981,14 +645,7 @@ __device__ __forceinline__ void attn_f32_body(const Params& p) {
     for (int v = 0; v < 4; ++v)
 #pragma unroll
       for (int c = 0; c < NC; ++c)
-        vf[v][c] = load_v4(pre, min(key0 + 4 * q4 + v, last), 64 * c + 4 * n,
-                           vsrc + (size_t)min(key0 + 4 * q4 + v, last) * D);
-    if constexpr (VIEW == 2) {
-      if (pre) {
-#pragma unroll
-        for (int ks = 0; ks < NKS; ++ks) kf[ks] = q4_f32x4(kcode[ks / 2] >> (16 * (ks & 1)), q4_scale(kscale));
-      }
-    }
+        vf[v][c] = load_f32x4(vsrc + (size_t)min(key0 + 4 * q4 + v, last) * D + 64 * c + 4 * n);
 
     f32x4 s[NR];  // scores of keys 4 * q4 + v
 #pragma unroll
@@ -999,14 +656,14 @@ __device__ __forceinline__ void attn_f32_body(const Params& p) {
       bf16x8 qf[NKS];
       const uint32_t qa = q_addr + r * 16 * QSTR * 4;
       qf[0] = lds_read_b128<0>(qa);
-      qf[1] = lds_read_b128<4 * KP>(qa);
-      qf[2] = lds_read_b128<8 * KP>(qa);
-      qf[3] = lds_read_b128<12 * KP>(qa);
+      qf[1] = lds_read_b128<64>(qa);
+      qf[2] = lds_read_b128<128>(qa);
+      qf[3] = lds_read_b128<192>(qa);
       if constexpr (NKS == 8) {
-        qf[4] = lds_read_b128<16 * KP>(qa);
-        qf[5] = lds_read_b128<20 * KP>(qa);
-        qf[6] = lds_read_b128<24 * KP>(qa);
-        qf[7] = lds_read_b128<28 * KP>(qa);
+        qf[4] = lds_read_b128<256>(qa);
+        qf[5] = lds_read_b128<320>(qa);
+        qf[6] = lds_read_b128<384>(qa);
+        qf[7] = lds_read_b128<448>(qa);
       }
       lds_wait<0>();
 #pragma unroll
@@ -1027,15 +684,8 @@ __device__ __forceinline__ void attn_f32_body(const Params& p) {
     __builtin_amdgcn_sched_barrier(0);
     if (i + NW < nt) load_k(i + NW);
     __builtin_amdgcn_sched_barrier(0);
-    bool masked = !pre || key0 + 16 > Pb;
-    // VIEW: not every key a sink or inside the last token's window
-    if constexpr (VIEW != 0) masked = masked || !(key0 + 16 <= p.sinks || key0 > Pb + t1 - p.window);
-    auto visible = [&](int r, int key) {
-      const bool shown = pre ? key < Pb : key >= vis_lo[r] && key < vis_hi[r];
-      if constexpr (VIEW != 0)
-        return shown && (key < p.sinks - (pre ? 0 : Pb) || key >= win_lo[r] + (pre ? Pb : 0));
-      return shown;
-    };
+    const bool masked = !pre || key0 + 16 > Pb;
+    auto visible = [&](int r, int key) { return pre ? key < Pb : key >= vis_lo[r] && key < vis_hi[r]; };
 #pragma unroll
     for (int r = 0; r < NR; ++r) {
       if (masked) {
@@ -1092,12 +742,12 @@ __device__ __forceinline__ void attn_f32_body(const Params& p) {
         for (int j = 0; j < 16; ++j) {
           const float pj = __shfl(j & 2 ? (j & 1 ? s[r][3] : s[r][2]) : (j & 1 ? s[r][1] : s[r][0]), 16 * (j >> 2) + n);
           if (!visible(r, key0 + j)) continue;
-          const float* vrow = vsrc + (size_t)min(key0 + j, last) * D;
+          const float* vrow = vsrc + (size_t)min(key0 + j, last) * D + 16 * q4;
 #pragma unroll
           for (int c = 0; c < NC; ++c)
 #pragma unroll
             for (int v = 0; v < 4; ++v) {
-              const f32x4 vv = load_v4(pre, min(key0 + j, last), 16 * q4 + 64 * c + 4 * v, vrow);
+              const f32x4 vv = load_f32x4(vrow + 64 * c + 4 * v);
 #pragma unroll
               for (int e = 0; e < 4; ++e) oacc[r][4 * c + e][v] = fmaf(pj, vv[e], oacc[r][4 * c + e][v]);
               __builtin_amdgcn_sched_barrier(0);
@@ -1148,17 +798,6 @@ __device__ __forceinline__ void attn_f32_body(const Params& p) {
   }
 }
 
-template <int D, int NR, int DS, int NW>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void slot_attn_f32_kernel(AttnParams32 p) {
-  attn_f32_body<D, NR, DS, NW, 0, AttnParams32>(p);
-}
-
-// The same kernel over a bounded view of the prefix.
-template <int D, int NR, int DS, int NW, int VIEW>
-__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void slot_view_f32_kernel(ViewParams32 p) {
-  attn_f32_body<D, NR, DS, NW, VIEW, ViewParams32>(p);
-}
-
 // ------------------------------------------------------------------ launchers
 
 template <int D>
@@ -1202,19 +841,6 @@ hipError_t launch_slot_attn_bf16(const AttnParams& p, int head_dim, hipStream_t 
   return hipGetLastError();
 }
 
-template <int D, int VIEW>
-void launch_view_as(const ViewParams& all, hipStream_t stream) {
-  for_each_view_launch(all, [&](const ViewParams& p) {
-    if (p.rows_per_block == kAttnWideRowsPerBlock) {
-      slot_view_bf16_kernel<D, 8, VIEW, 1><<<dim3(8 * p.per_xcd), dim3(512), 0, stream>>>(p);
-    } else if (p.key_groups == 2) {
-      slot_view_bf16_kernel<D, 4, VIEW, 2><<<dim3(8 * p.per_xcd), dim3(512), 0, stream>>>(p);
-    } else {
-      slot_view_bf16_kernel<D, 4, VIEW, 1><<<dim3(8 * p.per_xcd), dim3(256), 0, stream>>>(p);
-    }
-  });
-}
-
 hipError_t launch_slot_attn_merge(const AttnParams& p, int head_dim, hipStream_t stream) {
   if (head_dim == 128) {
     launch_attn_merge<128>(p, stream);
@@ -1224,75 +850,43 @@ hipError_t launch_slot_attn_merge(const AttnParams& p, int head_dim, hipStream_t
   return hipGetLastError();
 }
 
-hipError_t launch_slot_view_bf16(const ViewParams& p, int head_dim, bool codes, hipStream_t stream) {
-  if (codes) {
-    head_dim == 128 ? launch_view_as<128, 2>(p, stream) : launch_view_as<64, 2>(p, stream);
-  } else {
-    head_dim == 128 ? launch_view_as<128, 1>(p, stream) : launch_view_as<64, 1>(p, stream);
-  }
-  hipError_t e = hipGetLastError();
-  return e != hipSuccess || p.n_split == 1 ? e : launch_slot_attn_merge(p, head_dim, stream);
-}
-
-template <int VIEW, int D, int NR, int DS, int NW, class Params>
-void launch_attn_f32_as(Params p, int blocks, hipStream_t stream) {
+template <int D, int NR, int DS, int NW = kAttnF32Waves>
+void launch_attn_f32_as(AttnParams32 p, int blocks, hipStream_t stream) {
   const int64_t items = (int64_t)DS * blocks;
   for (int64_t i = 0; i < items; i += kAttnMaxGrid) {
     p.item0 = (int)i;
     const int n = (int)std::min<int64_t>(items - i, kAttnMaxGrid);
-    if constexpr (VIEW == 0) {
-      slot_attn_f32_kernel<D, NR, DS, NW><<<dim3(8 * ((n + 7) / 8)), dim3(NW * 64), 0, stream>>>(p);
-    } else {
-      slot_view_f32_kernel<D, NR, DS, NW, VIEW><<<dim3(8 * ((n + 7) / 8)), dim3(NW * 64), 0, stream>>>(p);
-    }
+    slot_attn_f32_kernel<D, NR, DS, NW><<<dim3(8 * ((n + 7) / 8)), dim3(NW * 64), 0, stream>>>(p);
   }
 }
 
-template <int VIEW, int NR, class Params>
-void launch_attn_f32_rows(const Params& p, int head_dim, int n_rb, hipStream_t stream) {
-  constexpr int NW = kAttnF32Waves;
+template <int NR>
+void launch_attn_f32_rows(const AttnParams32& p, int head_dim, int n_rb, hipStream_t stream) {
   const int blocks = p.B * p.Hkv * n_rb;
   if (head_dim == 64) {
-    launch_attn_f32_as<VIEW, 64, NR, 1, NW>(p, blocks, stream);
+    launch_attn_f32_as<64, NR, 1>(p, blocks, stream);
   } else if (NR == 1 && attn_f32_row_parts(head_dim, 16, blocks) == 2) {
-    launch_attn_f32_as<VIEW, 128, 1, 2, NW>(p, blocks, stream);
+    launch_attn_f32_as<128, 1, 2>(p, blocks, stream);
   } else {
-    launch_attn_f32_as<VIEW, 128, NR, 1, NW>(p, blocks, stream);
+    launch_attn_f32_as<128, NR, 1>(p, blocks, stream);
   }
-}
-
-// `prefix`: the prefix keys that a row block sees at most
-template <int VIEW, class Params>
-hipError_t launch_attn_f32(const Params& p, int head_dim, int64_t prefix, hipStream_t stream) {
-  const int R = p.G * p.T, rows = attn_f32_rows_per_block(p.B * (int64_t)p.Hkv, R, prefix + p.T);
-  if (attn_f32_one_wave(p.B * (int64_t)p.Hkv, R, attn_f32_keys_seen(prefix, p.T, p.L, p.cross))) {
-    const int blocks = p.B * p.Hkv * ((R + 15) / 16);
-    if (head_dim == 64) {
-      launch_attn_f32_as<VIEW, 64, 1, 1, 1>(p, blocks, stream);
-    } else {
-      launch_attn_f32_as<VIEW, 128, 1, 1, 1>(p, blocks, stream);
-    }
-    return hipGetLastError();
-  }
-  // 4-bit keys are read at an eighth of the bytes and stay with 16 rows (32 rows and
-  // the codes on their way do not fit the registers at D = 128)
-  if constexpr (VIEW != 2) {
-    if (rows == 32) {
-      launch_attn_f32_rows<VIEW, 2>(p, head_dim, (R + 31) / 32, stream);
-      return hipGetLastError();
-    }
-  }
-  launch_attn_f32_rows<VIEW, 1>(p, head_dim, (R + 15) / 16, stream);
-  return hipGetLastError();
 }
 
 hipError_t launch_slot_attn_f32(const AttnParams32& p, int head_dim, hipStream_t stream) {
-  return launch_attn_f32<0>(p, head_dim, p.P, stream);
-}
-
-hipError_t launch_slot_view_f32(const ViewParams32& p, int head_dim, bool codes, hipStream_t stream) {
-  const int64_t prefix = std::min<int64_t>(p.P, (int64_t)p.window + p.sinks);
-  return codes ? launch_attn_f32<2>(p, head_dim, prefix, stream) : launch_attn_f32<1>(p, head_dim, prefix, stream);
+  const int R = p.G * p.T, rows = attn_f32_rows_per_block(p.B * (int64_t)p.Hkv, R, (int64_t)p.P + p.T);
+  if (attn_f32_one_wave(p.B * (int64_t)p.Hkv, R, attn_f32_keys_seen(p.P, p.T, p.L, p.cross))) {
+    const int blocks = p.B * p.Hkv * ((R + 15) / 16);
+    if (head_dim == 64) {
+      launch_attn_f32_as<64, 1, 1, 1>(p, blocks, stream);
+    } else {
+      launch_attn_f32_as<128, 1, 1, 1>(p, blocks, stream);
+    }
+  } else if (rows == 32) {
+    launch_attn_f32_rows<2>(p, head_dim, (R + 31) / 32, stream);
+  } else {
+    launch_attn_f32_rows<1>(p, head_dim, (R + 15) / 16, stream);
+  }
+  return hipGetLastError();
 }
 
 }  // namespace zarya

@@ -1,0 +1,961 @@
+// Slot attention over a bounded view of the prefix (gfx950): a sliding window with
+// sinks, and a cache of 4-bit codes; see attn_view.hpp for what is visible and for the
+// code's format, slot_attn_few.hip for few query rows.
+//
+// The tile loop is slot_attn.hip's, whose comments are not repeated here: 64-key tiles
+// in XOR-swizzled LDS, S^T = K Q^T, O^T += V^T P^T with the scores as the B operand
+// as they stand, one tile ahead.  (A kernel of its own: with the views' choices in one
+// template the whole-prefix kernels came out 1.5 to 3% slower.)  What differs:
+//  * The tiles are those of a list (KeyTiles), shared out among the splits by their
+//    number in the batch row at hand.
+//  * 4-bit tiles come through registers: codes and scales requested two tiles ahead,
+//    converted (exactly) into the tile's bf16 image in LDS one tile ahead.
+//  * Two groups of four waves may hold the same 128 rows and take half of the tiles
+//    each, where row blocks alone would leave a SIMD one wave.
+//  * The visible keys of a masked tile are one 64-bit word per row, and a value that a
+//    row does not see never reaches it, infinities and NaN included.
+#include <algorithm>
+#include <type_traits>
+#include <utility>
+
+#include "attn_view.hpp"
+#include "common.hpp"
+#include "kernels.hpp"
+
+namespace zarya {
+
+namespace {
+
+// f(std::integral_constant<int, 0>{}) ... f(std::integral_constant<int, N - 1>{})
+template <class F, int... I>
+__device__ __forceinline__ void static_for(std::integer_sequence<int, I...>, F&& f) {
+  (f(std::integral_constant<int, I>{}), ...);
+}
+template <int N, class F>
+__device__ __forceinline__ void static_for(F&& f) {
+  static_for(std::make_integer_sequence<int, N>{}, f);
+}
+
+constexpr int KT = 64;          // keys per tile
+constexpr float kRescaleLog2 = 8.f;  // growth of a row maximum (log2 units) that forces a rescale
+
+// XOR swizzle of the 16-byte chunk index of LDS row `kr`, as in slot_attn.hip.
+template <int D>
+__host__ __device__ constexpr int swz(int kr) {
+  if constexpr (D == 128) {
+    return ((kr & 7) << 1) | ((kr >> 3) & 1);
+  } else {
+    return (((kr >> 1) & 3) << 1) | ((kr >> 3) & 1);
+  }
+}
+
+}  // namespace
+
+// NWAVE: waves of a group, 32 query rows each; GRP: groups.  CODES: the caches hold
+// 4-bit codes.
+template <int D, int NWAVE, bool CODES, int GRP>
+__global__ __launch_bounds__(NWAVE * GRP * 64) __attribute__((amdgpu_waves_per_eu(2))) void slot_view_bf16_kernel(
+    ViewParams p) {
+  constexpr int RB = NWAVE * 32;        // query rows per workgroup
+  constexpr int ROWB = D * 2;           // bytes per key row
+  constexpr int TILEB = KT * ROWB;      // bytes of one K (or V) tile
+  constexpr int CPW = TILEB / 1024 / NWAVE;  // 1 KB direct loads per wave per tile (K; same for V)
+  constexpr int LPR = ROWB / 16;        // lanes per row in a direct load
+  constexpr int RPC = 1024 / ROWB;      // rows per 1 KB chunk
+  constexpr int NDB = D / 32;           // 32-wide blocks of the head dim
+  constexpr int NKS = D / 16;           // k-steps of the QK^T contraction
+  static_assert(CPW * NWAVE * 1024 == TILEB, "tile must split into 1 KB chunks per wave");
+  __shared__ __attribute__((aligned(16))) uint8_t lds_all[GRP][2][2][TILEB];
+
+  int rb, split, bg;  // row block, prefix split, b * Hkv + g
+  if (p.heavy_first) {
+    // Causal launch whose XCDs each hold whole GQA groups (one split): an
+    // XCD walks its groups' row blocks heaviest first (the last tokens see
+    // the most keys), so the longest work items start first and the short
+    // ones fill the tail.
+    const int x = blockIdx.x & 7, k = blockIdx.x >> 3;
+    const int gpx = p.per_xcd / p.n_rb;  // groups per XCD
+    rb = p.n_rb - 1 - k / gpx;
+    split = 0;
+    bg = x * gpx + k % gpx;
+  } else {
+    int w = xcd_work_index(blockIdx.x, p.per_xcd, p.n_items);
+    if (w < 0) return;
+    w += p.item0;
+    rb = w % p.n_rb;
+    split = (w / p.n_rb) % p.n_split;
+    bg = w / (p.n_rb * p.n_split);
+  }
+  const int b = bg / p.Hkv;
+  // this batch row's prefix length (rows differ after KV-cache appends)
+  const int Pb = p.prefix_lens ? min(max(p.prefix_lens[b], 0), p.P) : p.P;
+
+  const int tid = threadIdx.x;
+  const int lane = tid & 63, wave = tid >> 6;
+  const int wave_all = __builtin_amdgcn_readfirstlane(wave);
+  // GRP > 1: groups of NWAVE waves hold the same rows and take a share of the
+  // tiles each, with LDS buffers of their own
+  const int grp = GRP > 1 ? wave_all / NWAVE : 0;
+  const int wave_u = GRP > 1 ? wave_all % NWAVE : wave_all;
+  auto& lds = lds_all[grp];
+  const int n = lane & 31, hh = lane >> 5;
+
+  // ---- this lane's query row and its visible range [vis_lo, vis_hi) of
+  // draft-token keys.  A group's G*T rows are taken token-major (row = t*G +
+  // h), so a block's rows cover a contiguous token range of every head of
+  // the group and share one visible key range; mrow is the row's place in
+  // the head-major [G, T] layout of q and out.
+  const int row = rb * RB + (GRP > 1 ? wave_u : wave) * 32 + n;
+  const bool row_ok = row < p.R;
+  const int mrow = (row % p.G) * p.T + row / p.G;
+  int vis_lo = 0, vis_hi = 0;
+  int win_lo = 0;  // the first draft key inside the row's window
+  if (row_ok) {
+    const int t = row / p.G;
+    win_lo = t - p.window + 1;
+    const int s = t / p.L, r = t - s * p.L;
+    const int pass = p.slot_pass ? (int)p.slot_pass[b * p.S + s] : p.pass;
+    const int own_lo = s * p.L;
+    vis_hi = own_lo + (pass == 0 ? p.L : r + 1);
+    vis_lo = p.cross ? 0 : own_lo;
+  }
+
+  // ---- Q fragments (B operand of S^T = K Q^T), requested before the tiles are worked
+  // out and waited for with the first
+  bf16x8 qf[NKS];
+  {
+    const uint4* qrow = reinterpret_cast<const uint4*>(p.q + ((size_t)bg * p.R + (row_ok ? mrow : 0)) * D);
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {
+      uint4 v = row_ok ? qrow[2 * ks + hh] : make_uint4(0, 0, 0, 0);
+      qf[ks] = __builtin_bit_cast(bf16x8, v);
+    }
+  }
+
+  // ---- key tiles of this workgroup: the listed tiles of the block's tokens are shared
+  // out among the splits, tile i of this group being the list's first + i.  tw0..tw1:
+  // this wave's tokens.
+  KeyTiles<KT> tiles;
+  const int t0 = rb * RB / p.G, t1 = (min(p.R, rb * RB + RB) - 1) / p.G;
+  tiles.list(Pb, t0, p.cross ? 0 : t0 / p.L * p.L,
+             p.pass != 0 && !p.slot_pass ? t1 + 1 : min(p.T, (t1 / p.L + 1) * p.L), p.window, p.sinks);
+  const int per_split = (tiles.nt + p.n_split - 1) / p.n_split;
+  int first = min(split * per_split, tiles.nt);
+  int nt = min(per_split, tiles.nt - first);
+  const int steps = (nt + GRP - 1) / GRP;  // tiles of the group that has the most
+  if constexpr (GRP > 1) {
+    const int skip = min(grp * steps, nt);
+    first += skip;
+    nt = min(steps, nt - skip);
+  }
+  const int tw0 = (rb * RB + wave_u * 32) / p.G, tw1 = (min(p.R, rb * RB + wave_u * 32 + 32) - 1) / p.G;
+  auto is_pre = [&](int i) { return first + i < tiles.n_pre; };
+
+  // ---- direct-to-LDS staging of K and V tiles: load j of a wave fills 1 KB
+  // chunk c = NWAVE*j + wave (RPC rows); lane l lands at row RPC*c + l/LPR,
+  // physical 16-byte column l%LPR and fetches the logical column the swizzle
+  // puts there.  Rows past the valid keys are clamped to the last valid row
+  // (their scores are masked, so they contribute exact zeros).
+  int my_r[CPW];
+  uint32_t my_off[CPW];
+#pragma unroll
+  for (int j = 0; j < CPW; ++j) {
+    my_r[j] = RPC * (NWAVE * j + wave_u) + lane / LPR;
+    my_off[j] = (uint32_t)(my_r[j] * ROWB + (((lane % LPR) ^ swz<D>(my_r[j])) << 4));
+  }
+  const char* kc = reinterpret_cast<const char*>(p.k_cache + (size_t)bg * p.C * D);
+  const char* vc = reinterpret_cast<const char*>(p.v_cache + (size_t)bg * p.C * D);
+  const char* ks_ = reinterpret_cast<const char*>(p.k_slot + (size_t)bg * p.T * D);
+  const char* vs_ = reinterpret_cast<const char*>(p.v_slot + (size_t)bg * p.T * D);
+  auto issue = [&](int i, int buf) __attribute__((always_inline)) {
+    const bool pre = !CODES && is_pre(i);
+    const int key0 = tiles.key0(first + i), valid = (pre ? Pb : p.T) - key0;
+    const char* kp = (pre ? kc : ks_) + (size_t)key0 * ROWB;
+    const char* vp = (pre ? vc : vs_) + (size_t)key0 * ROWB;
+    uint8_t* kd = &lds[buf][0][wave_u * 1024];
+    uint8_t* vd = &lds[buf][1][wave_u * 1024];
+    if (valid >= KT) {
+#pragma unroll
+      for (int j = 0; j < CPW; ++j) {
+        dma16(kp + my_off[j], kd + NWAVE * j * 1024);
+        dma16(vp + my_off[j], vd + NWAVE * j * 1024);
+      }
+    } else {
+#pragma unroll
+      for (int j = 0; j < CPW; ++j) {
+        const int dr = min(my_r[j], valid - 1) - my_r[j];  // <= 0: clamp to the last valid row
+        dma16(kp + my_off[j] + dr * ROWB, kd + NWAVE * j * 1024);
+        dma16(vp + my_off[j] + dr * ROWB, vd + NWAVE * j * 1024);
+      }
+    }
+  };
+
+  // ---- 4-bit tiles: a block of 32 codes (16 bytes) and its scale byte per
+  // thread and piece, requested two tiles ahead into registers and converted into
+  // the tile's bf16 image in LDS one tile ahead
+  constexpr int NB = D / 32;                             // blocks per row
+  constexpr int NPC = 2 * KT * NB;                       // K's pieces, then V's
+  constexpr int PCS = (NPC + NWAVE * 64 - 1) / (NWAVE * 64);  // per thread
+  uint4 codes[PCS];
+  uint32_t scales[PCS];
+  auto piece = [&](int j, int& which, int& r, int& blk) __attribute__((always_inline)) {
+    const int c0 = wave_u * 64 + j * NWAVE * 64;  // wave-uniform; KT * NB is a multiple of 64
+    which = c0 / (KT * NB);
+    const int c = c0 % (KT * NB) + lane;
+    r = c / NB;
+    blk = c % NB;
+    return c0 < NPC;
+  };
+  auto fetch_q4 = [&](int i) __attribute__((always_inline)) {
+    if constexpr (CODES) {
+      const int key0 = tiles.key0(first + i);
+      const size_t base = (size_t)bg * p.C + key0;
+#pragma unroll
+      for (int j = 0; j < PCS; ++j) {
+        int which, r, blk;
+        if (!piece(j, which, r, blk)) continue;
+        r = min(r, Pb - key0 - 1);  // rows past the valid keys follow the last one
+        const uint8_t* cp = reinterpret_cast<const uint8_t*>(which ? p.v_cache : p.k_cache) + base * (D / 2);
+        const uint8_t* sp = (which ? p.v_scale : p.k_scale) + base * NB;
+        codes[j] = *reinterpret_cast<const uint4*>(cp + (uint32_t)(r * (D / 2) + blk * 16));
+        scales[j] = sp[(uint32_t)(r * NB + blk)];
+      }
+    }
+  };
+  auto unpack_q4 = [&](int buf) __attribute__((always_inline)) {
+#pragma unroll
+    for (int j = 0; j < PCS; ++j) {
+      int which, r, blk;
+      if (!piece(j, which, r, blk)) continue;
+      uint8_t* dst = &lds[buf][which][r * ROWB];
+      const float sc = q4_scale(scales[j]);
+      const uint32_t cw[4] = {codes[j].x, codes[j].y, codes[j].z, codes[j].w};
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        *reinterpret_cast<bf16x8*>(dst + (((4 * blk + e) ^ swz<D>(r)) << 4)) = q4_bf16x8(cw[e], sc);
+    }
+  };
+  // tile j into buffer buf: its codes are in registers, or it is loaded directly
+  auto advance = [&](int j, int buf) __attribute__((always_inline)) {
+    if (j >= nt) return;
+    if (is_pre(j)) {
+      unpack_q4(buf);
+    } else {
+      issue(j, buf);
+    }
+    if (j + 1 < nt && is_pre(j + 1)) fetch_q4(j + 1);
+  };
+
+  f32x16 oacc[NDB];
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) oacc[db] = f32x16{};
+  float m_run = kNegBig, l_run = 0.f;  // running max of raw scores; sum of 2^(scaled score - scaled max)
+  const float c2 = p.scale_log2;
+
+  // lane-dependent parts of the LDS fragment addresses (the swizzle of every
+  // row a lane reads depends on the lane only)
+  const uint32_t lds0 = lds_addr(&lds[0][0][0]);
+  // K fragment of k-step ks: row n, logical chunk 2*ks + hh, i.e. physical
+  // chunk (2*ks) ^ (hh ^ swz(n)) (2*ks is even, hh the low bit)
+  const uint32_t k_row = lds0 + n * ROWB;
+  const uint32_t k_cx = (uint32_t)((hh ^ swz<D>(n)) << 4);
+  uint32_t k_addr[NKS];
+#pragma unroll
+  for (int ks = 0; ks < NKS; ++ks) k_addr[ks] = k_row + (k_cx ^ ((uint32_t)ks << 5));
+  const int q16 = lane >> 4, rr = lane & 15;
+  const int vrow = 4 * hh + (rr >> 2);  // first key row of this lane's transposing reads (+16*st, +8)
+  // Rows vrow + 16 * step and vrow + 8 + 16 * step: the swizzle repeats every
+  // 16 rows and, for vrow < 8, swz(vrow + 8) = swz(vrow) ^ 1, which flips bit
+  // 4 of the address (the chunk's low bit): the second half of a step is read
+  // at (v_col ^ 16) + 8 rows.
+  uint32_t v_addr[NDB][2];  // first and second half-step
+#pragma unroll
+  for (int db = 0; db < NDB; ++db) {
+    const int d = db * 32 + (q16 & 1) * 16 + 4 * (rr & 3);
+    const uint32_t v_col = vrow * ROWB + (((d >> 3) ^ swz<D>(vrow)) << 4) + (d & 7) * 2;
+    v_addr[db][0] = lds0 + TILEB + v_col;
+    v_addr[db][1] = lds0 + TILEB + (v_col ^ 16u) + 8 * ROWB;
+  }
+  static_assert((swz<D>(8) ^ swz<D>(0)) == 1, "second V half-step addressing assumes swz(r + 8) = swz(r) ^ 1");
+
+  f32x16 sacc[2];   // scores of the tile between its QK^T and its softmax
+  bf16x8 pb[4];      // its probabilities (bf16, B operands of the PV steps)
+  v4i16 vf[2][NDB][2];  // V^T fragments, double-buffered across PV steps
+
+  // ---- S^T = K Q^T of tile i for two 32-key blocks; register v of block kb
+  // holds key kb*32 + 8*(v/4) + 4*hh + v%4 of the tile.  K fragments are read
+  // one k-step ahead of their MFMAs (deeper read-ahead measured no faster).
+  auto qk = [&](auto buf) __attribute__((always_inline)) {
+    constexpr int KB = decltype(buf)::value * 2 * TILEB;
+    sacc[0] = f32x16{};
+    sacc[1] = f32x16{};
+    bf16x8 kf[2][2];
+    kf[0][0] = lds_read_b128<KB>(k_addr[0]);
+    kf[0][1] = lds_read_b128<KB + 32 * ROWB>(k_addr[0]);
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) {
+      const int sl = ks & 1;
+      if (ks + 1 < NKS) {
+        kf[sl ^ 1][0] = lds_read_b128<KB>(k_addr[ks + 1]);
+        kf[sl ^ 1][1] = lds_read_b128<KB + 32 * ROWB>(k_addr[ks + 1]);
+        lds_wait<2>();
+      } else {
+        lds_wait<0>();
+      }
+      lds_tie(kf[sl][0]);
+      lds_tie(kf[sl][1]);
+      sacc[0] = mfma32x32x16(kf[sl][0], qf[ks], sacc[0]);
+      sacc[1] = mfma32x32x16(kf[sl][1], qf[ks], sacc[1]);
+    }
+  };
+
+  // ---- V^T fragments of PV step `stp` of a tile
+  auto pv_read = [&](auto buf, auto stp) __attribute__((always_inline)) {
+    constexpr int OFF = decltype(buf)::value * 2 * TILEB + 16 * decltype(stp)::value * ROWB;
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) {
+      vf[decltype(stp)::value & 1][db][0] = lds_read_tr16_b64<OFF>(v_addr[db][0]);
+      vf[decltype(stp)::value & 1][db][1] = lds_read_tr16_b64<OFF>(v_addr[db][1]);
+    }
+  };
+
+  // ---- online softmax of tile i's scores; masks only on tiles that need them
+  auto softmax = [&](int i) __attribute__((always_inline)) {
+    const bool is_slot = !is_pre(i);
+    const int key0 = tiles.key0(first + i);
+    // nothing to hide: every key shown to every token of the wave by the pass, and
+    // all of them sinks or inside the last token's window
+    const int off = is_slot ? 0 : Pb;  // places of the tile's keys less their indices, as seen from the tokens
+    const int sink_hi = is_slot ? p.sinks - Pb : p.sinks;
+    const bool shown = is_slot ? key0 >= (p.cross ? 0 : tw1 / p.L * p.L) && key0 + KT <= tw0 + 1 : key0 + KT <= Pb;
+    const bool masked = !(shown && (key0 + KT <= sink_hi || key0 > off + tw1 - p.window));
+    if (masked) {
+      // the row's keys as bits: below(x), the tile's keys under x
+      auto below = [&](int x) { return x <= key0 ? 0ull : x - key0 >= KT ? ~0ull : (1ull << (x - key0)) - 1; };
+      const uint64_t range = is_slot ? below(vis_hi) & ~below(vis_lo) : below(Pb);
+      const uint64_t m = range & (below(sink_hi) | ~below(win_lo + off));
+      const uint32_t seen[2] = {(uint32_t)m >> (4 * hh), (uint32_t)(m >> 32) >> (4 * hh)};
+#pragma unroll
+      for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+        for (int v = 0; v < 16; ++v)
+          if (!(seen[kb] >> (8 * (v >> 2) + (v & 3)) & 1)) sacc[kb][v] = -INFINITY;
+    }
+    // tile maximum of this lane's row: a max3 tree (depth 3 instead of a
+    // 16-long chain), then the other lane half of the row
+    float mt;
+    {
+      float t[11];
+#pragma unroll
+      for (int j = 0; j < 5; ++j) t[j] = max3f(sacc[0][3 * j], sacc[0][3 * j + 1], sacc[0][3 * j + 2]);
+      t[5] = max3f(sacc[0][15], sacc[1][0], sacc[1][1]);
+#pragma unroll
+      for (int j = 0; j < 4; ++j) t[6 + j] = max3f(sacc[1][3 * j + 2], sacc[1][3 * j + 3], sacc[1][3 * j + 4]);
+      t[10] = max3f(sacc[1][14], sacc[1][15], sacc[1][15]);
+      const float u0 = max3f(t[0], t[1], t[2]), u1 = max3f(t[3], t[4], t[5]);
+      const float u2 = max3f(t[6], t[7], t[8]), u3 = max3f(t[9], t[10], t[10]);
+      mt = max_xor32(max3f(max3f(u0, u1, u2), u3, u3));
+    }
+    const float m_new = fmaxf(m_run, mt);
+    // Rescale only when the maximum of some row moved by more than 2^8 in
+    // probability: until then the exponentials below are taken against the
+    // stale maximum and stay <= 2^8 (exact in the float32 sums, same relative
+    // rounding in bf16), and the final O / l and LSE do not depend on which
+    // maximum was used.  Random scores raise a row's maximum on most early
+    // tiles, each time by little; this skips those rescales.  Every PV of the
+    // earlier tiles is in oacc before this (the callers keep that order).
+    if (__any((m_new - m_run) * c2 > kRescaleLog2)) {
+      const float alpha = fast_exp2((m_run - m_new) * c2);
+      l_run *= alpha;
+#pragma unroll
+      for (int db = 0; db < NDB; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) oacc[db][v] *= alpha;
+      m_run = m_new;
+    }
+    const float mc = m_run * c2;
+    float ps[4] = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int kb = 0; kb < 2; ++kb)
+#pragma unroll
+      for (int half = 0; half < 2; ++half) {
+        uint32_t pk[4];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+          const int v = half * 8 + j;
+          const float e0 = fast_exp2(fmaf(sacc[kb][v], c2, -mc));
+          const float e1 = fast_exp2(fmaf(sacc[kb][v + 1], c2, -mc));
+          ps[j >> 1] += e0 + e1;
+          pk[j >> 1] = pack_bf16x2_hw(e0, e1);
+        }
+        // B operand of PV step 2*kb + half: slot j = accumulator register 8*half + j
+        pb[2 * kb + half] = __builtin_bit_cast(bf16x8, make_uint4(pk[0], pk[1], pk[2], pk[3]));
+      }
+    l_run += (ps[0] + ps[1]) + (ps[2] + ps[3]);
+  };
+
+  // ---- O^T += V^T P^T of tile i (after pv_read of step 0).  Step st covers
+  // keys 16*st + 4*hh + {0..3} (slots 0-3) and 16*st + 8 + 4*hh + {0..3} (slots
+  // 4-7); V^T fragments are read one step ahead with the transposing LDS read.
+  auto pv = [&](auto buf) __attribute__((always_inline)) {
+    static_for<4>([&](auto stp) __attribute__((always_inline)) {
+      constexpr int st = decltype(stp)::value;
+      if constexpr (st + 1 < 4) {
+        pv_read(buf, std::integral_constant<int, st + 1>{});
+        lds_wait<2 * NDB>();
+      } else {
+        lds_wait<0>();
+      }
+#pragma unroll
+      for (int db = 0; db < NDB; ++db) {
+        v4i16(&f)[2] = vf[st & 1][db];
+        lds_tie(f[0]);
+        lds_tie(f[1]);
+        const uint2 l2 = __builtin_bit_cast(uint2, f[0]);
+        const uint2 h2 = __builtin_bit_cast(uint2, f[1]);
+        const bf16x8 a = __builtin_bit_cast(bf16x8, make_uint4(l2.x, l2.y, h2.x, h2.y));
+        oacc[db] = mfma32x32x16(a, pb[st], oacc[db]);
+      }
+    });
+  };
+
+  // The LDS buffer of a tile is a compile-time constant of its half of the
+  // loop, so that every fragment address is a register set up once plus an
+  // immediate offset (the 40 additions per tile it saves are a tenth of the
+  // vector instructions beside the MFMAs, and the two hardly overlap: the 4B
+  // shape 308 -> 294 us, the training layout 672 -> 651, 1.7B 118 -> 115.5; at
+  // 0.6B, 42.1 us, no difference).
+  // a wave of padding rows only helps to load the tiles (520 rows a group in
+  // blocks of 128, Mode A: the step 211 -> 207 us)
+  const bool live = rb * RB + wave_u * 32 < p.R;
+  constexpr std::integral_constant<int, 0> c0{};
+  constexpr std::integral_constant<int, 1> c1{};
+  auto step = [&](int i, auto buf) __attribute__((always_inline)) {
+    wait_vmcnt<0>();
+    block_barrier();
+    if constexpr (CODES) {
+      advance(i + 1, decltype(buf)::value ^ 1);
+    } else {
+      if (i + 1 < nt) issue(i + 1, decltype(buf)::value ^ 1);
+    }
+    if (!live || (GRP > 1 && i >= nt)) return;
+    qk(buf);
+    pv_read(buf, std::integral_constant<int, 0>{});  // in flight during the softmax
+    softmax(i);
+    pv(buf);
+  };
+  if constexpr (CODES) {
+    if (nt > 0 && is_pre(0)) fetch_q4(0);
+    advance(0, 0);
+  } else {
+    if (nt > 0) issue(0, 0);
+  }
+  // the queries are waited for here: in the loop it would be with every tile's loads
+#pragma unroll
+  for (int ks = 0; ks < NKS; ++ks) lds_tie(qf[ks]);
+  for (int i = 0; i < steps; i += 2) {
+    step(i, c0);
+    if (i + 1 < steps) step(i + 1, c1);
+  }
+
+  // A value that is not finite has left its mark on the sums of every row whose
+  // tile held it, seen or not (0 * inf).  Then the wave's sums are taken once
+  // more, key by key over the visible ones (the maxima and the sums of the
+  // probabilities never saw the others).
+  float z = 0.f;
+#pragma unroll
+  for (int db = 0; db < NDB; ++db)
+#pragma unroll
+    for (int v = 0; v < 16; ++v) z = fmaf(oacc[db][v], 0.f, z);
+  if (__any(row_ok && z != 0.f)) {
+#pragma unroll
+    for (int db = 0; db < NDB; ++db) oacc[db] = f32x16{};
+    // eight elements from d on of a row of K (which = 0) or V
+    auto row8 = [&](bool pre, int which, int key, int d) __attribute__((always_inline)) {
+      if (CODES && pre) {
+        const size_t at = (size_t)bg * p.C + key;
+        const uint8_t* cp = reinterpret_cast<const uint8_t*>(which ? p.v_cache : p.k_cache) + at * (D / 2) + d / 2;
+        return q4_bf16x8(*reinterpret_cast<const uint32_t*>(cp),
+                         q4_scale((which ? p.v_scale : p.k_scale)[at * NB + d / 32]));
+      }
+      const char* base = pre ? (which ? vc : kc) : which ? vs_ : ks_;
+      return *reinterpret_cast<const bf16x8*>(base + (size_t)key * ROWB + d * 2);
+    };
+    const uint16_t* qrow = p.q + ((size_t)bg * p.R + (row_ok ? mrow : 0)) * D;
+#pragma unroll 1
+    for (int i = 0; i < nt; ++i) {
+      const bool pre = is_pre(i);
+      const int key0 = tiles.key0(first + i), end = min(key0 + KT, pre ? Pb : p.T);
+      const int off = pre ? Pb : 0;
+#pragma unroll 1
+      for (int key = key0; key < end; ++key) {
+        const bool ok = row_ok && (pre || (key >= vis_lo && key < vis_hi)) &&
+                        (key < p.sinks - (pre ? 0 : Pb) || key >= win_lo + off);
+        if (!__any(ok)) continue;
+        float sc = 0.f;
+#pragma unroll 1
+        for (int c = 0; c < D / 2; c += 8) {
+          const int d = hh * (D / 2) + c;
+          const bf16x8 qv = *reinterpret_cast<const bf16x8*>(qrow + d), kv = row8(pre, 0, key, d);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) sc = fmaf((float)qv[e], (float)kv[e], sc);
+        }
+        sc = sum_xor32(sc);
+        const float pr = (float)(__bf16)fast_exp2(fmaf(sc, c2, -(m_run * c2)));
+#pragma unroll
+        for (int db = 0; db < NDB; ++db)
+#pragma unroll
+          for (int u = 0; u < 4; ++u) {
+            const bf16x8 vv = row8(pre, 1, key, db * 32 + 8 * u);
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+              const float x = hh ? (float)vv[4 + e] : (float)vv[e];
+              oacc[db][4 * u + e] = ok ? fmaf(pr, x, oacc[db][4 * u + e]) : oacc[db][4 * u + e];
+            }
+            __builtin_amdgcn_sched_barrier(0);  // one piece at a time: no more registers than the loop above
+          }
+      }
+    }
+  }
+
+  // ---- finalize.  Of two groups each takes half of the rows' elements and gets the
+  // other's sums of them, lane by lane through the tile buffers.
+  constexpr int DBG = NDB / GRP;  // 32-wide blocks taken
+  constexpr int XW = (DBG * 16 + 2) * 64;  // words that a wave is given
+  static_assert(GRP <= 2 && (GRP == 1 || GRP * NWAVE * XW * 4 <= (int)sizeof lds_all), "room for the sums");
+  const int d0 = grp * DBG * 32;
+  float* words = reinterpret_cast<float*>(&lds_all[0][0][0][0]);
+  f32x16 fin[DBG];
+  float m_fin = m_run, l_fin = l_run;
+  __syncthreads();  // every wave is done with the tiles
+  auto halves = [&](auto own) __attribute__((always_inline)) {
+    constexpr int MINE = decltype(own)::value * DBG, OTHER = NDB - DBG - MINE;
+    if constexpr (GRP > 1) {
+      float* to = words + ((grp ^ 1) * NWAVE + wave_u) * XW + lane;
+      const float* from = words + (grp * NWAVE + wave_u) * XW + lane;
+#pragma unroll
+      for (int db = 0; db < DBG; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) to[(db * 16 + v) * 64] = oacc[OTHER + db][v];
+      to[DBG * 16 * 64] = m_run;
+      to[(DBG * 16 + 1) * 64] = l_run;
+      __syncthreads();
+      const float m1 = from[DBG * 16 * 64], l1 = from[(DBG * 16 + 1) * 64];
+      m_fin = fmaxf(m_run, m1);
+      const float a0 = fast_exp2((m_run - m_fin) * c2), a1 = fast_exp2((m1 - m_fin) * c2);
+      l_fin = l_run * a0 + l1 * a1;
+#pragma unroll
+      for (int db = 0; db < DBG; ++db)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) fin[db][v] = oacc[MINE + db][v] * a0 + from[(db * 16 + v) * 64] * a1;
+    } else {
+#pragma unroll
+      for (int db = 0; db < DBG; ++db) fin[db] = oacc[db];
+    }
+  };
+  if (grp == 0) {
+    halves(c0);
+  } else if constexpr (GRP > 1) {
+    halves(c1);
+  }
+  const float l_tot = sum_xor32(l_fin);
+  const float inv = l_tot > 0.f ? 1.f / l_tot : 0.f;
+  const float lse2 = m_fin * c2 + __log2f(l_tot);  // log2 units
+  const size_t grow0 = (size_t)bg * p.R;
+  if (p.n_split == 1) {
+    // rows of the output by 16 neighbouring bytes a lane, turned in an LDS piece of the
+    // wave's own (training layout under a window of 1024, with the queries requested
+    // first: 326 -> 308 us; 1.7B verification over 4-bit keys 29.9 -> 27.6)
+    constexpr int CH = DBG * 4;  // 16-byte pieces of a row
+    uint8_t* own = reinterpret_cast<uint8_t*>(words) + (grp * NWAVE + wave_u) * (GRP > 1 ? XW * 4 : 32 * CH * 16);
+#pragma unroll
+    for (int db = 0; db < DBG; ++db)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) {
+        uint2 pk;
+        pk.x = pack_bf16x2_hw(fin[db][4 * u] * inv, fin[db][4 * u + 1] * inv);
+        pk.y = pack_bf16x2_hw(fin[db][4 * u + 2] * inv, fin[db][4 * u + 3] * inv);
+        *reinterpret_cast<uint2*>(own + n * (CH * 16) + (((db * 4 + u) ^ (n & (CH - 1))) << 4) + hh * 8) = pk;
+      }
+    asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");  // the wave's writes before its reads
+#pragma unroll
+    for (int i = 0; i < CH / 2; ++i) {
+      const int r = i * (64 / CH) + lane / CH, c = lane % CH;
+      const uint4 v = *reinterpret_cast<const uint4*>(own + r * (CH * 16) + ((c ^ (r & (CH - 1))) << 4));
+      const int at = __shfl(row_ok ? mrow : -1, r);
+      if (at >= 0) *reinterpret_cast<uint4*>(p.out + (grow0 + at) * D + d0 + 8 * c) = v;
+    }
+    if (p.lse && hh == 0 && grp == 0 && row_ok) p.lse[grow0 + mrow] = lse2 * kLn2;
+  } else if (row_ok) {
+    const size_t prow = (size_t)split * p.rows_total + grow0 + mrow;
+#pragma unroll
+    for (int db = 0; db < DBG; ++db)
+#pragma unroll
+      for (int u = 0; u < 4; ++u)
+        *reinterpret_cast<float4*>(p.part_o + prow * D + d0 + db * 32 + 8 * u + 4 * hh) =
+            make_float4(fin[db][4 * u] * inv, fin[db][4 * u + 1] * inv, fin[db][4 * u + 2] * inv,
+                        fin[db][4 * u + 3] * inv);
+    if (hh == 0 && grp == 0) p.part_lse[prow] = l_tot > 0.f ? lse2 : -INFINITY;
+  }
+}
+
+// float32: slot_attn_f32_kernel's design (its comments hold here too) over the listed
+// tiles of 16 keys.  With 4-bit codes the contraction is taken in another order, in
+// which a lane's elements of a key are one run: a quarter of the row.
+template <int D, int NR, int DS, int NW, bool CODES>
+__global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) void slot_view_f32_kernel(ViewParams32 p) {
+  constexpr int RB = 16 * NR;   // query rows per workgroup
+  constexpr int NKS = D / 16;   // 16-byte pieces of a K row per lane
+  constexpr int DO = D / DS;    // elements of the output row taken by this workgroup
+  constexpr int NC = DO / 64;   // 16-byte pieces of a V row per lane
+  constexpr int NOB = DO / 16;  // 16-wide blocks of the output: block 4 * c + e holds d = 64 * c + 4 * i + e
+  constexpr int OSTR = DO + 4;  // row stride of the partial outputs in LDS
+  constexpr int QSTR = D + 4;   // and of the queries
+  constexpr int KQ = CODES ? D / 4 : 4;   // element of a lane's first K piece, per lane quarter
+  constexpr int KP = CODES ? 4 : 16;      // from one piece to the next
+  __shared__ __attribute__((aligned(16))) float part_o[NW][RB][OSTR];
+  __shared__ __attribute__((aligned(16))) float qs[RB][QSTR];  // scaled queries; the padding spreads the rows over the banks
+  __shared__ float part_m[NW][RB], part_l[NW][RB];
+
+  const int n_rb = (p.G * p.T + RB - 1) / RB;
+  const int w = xcd_work_index(blockIdx.x, gridDim.x >> 3, min(p.B * p.Hkv * n_rb * DS - p.item0, kAttnMaxGrid)) + p.item0;
+  if (w < p.item0) return;
+  const int d0 = (w % DS) * DO;  // first element taken
+  const int rb = w / DS % n_rb, bg = w / (DS * n_rb);
+  const int b = bg / p.Hkv;
+  const int R = p.G * p.T;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int n = lane & 15, q4 = lane >> 4;
+  const int Pb = p.prefix_lens ? min(max(p.prefix_lens[b], 0), p.P) : p.P;
+
+  // this lane's query rows (one per row tile) and their visible draft keys;
+  // rows past the end follow the last one and are not stored
+  int vis_lo[NR], vis_hi[NR];
+  int win_lo[NR];  // the first draft key inside the row's window
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    const int row = min(rb * RB + 16 * r + n, R - 1);
+    const int t = row / p.G, s = t / p.L;
+    win_lo[r] = t - p.window + 1;
+    const int pass = p.slot_pass ? (int)p.slot_pass[b * p.S + s] : p.pass;
+    vis_hi[r] = pass == 0 ? (s + 1) * p.L : t + 1;
+    vis_lo[r] = p.cross ? 0 : s * p.L;
+  }
+  for (int x = threadIdx.x; x < RB * (D / 4); x += NW * 64) {
+    const int lr = x / (D / 4), c = 4 * (x % (D / 4));
+    const int row = min(rb * RB + lr, R - 1);
+    const size_t qr = (size_t)bg * R + (size_t)(row % p.G) * p.T + row / p.G;
+    *reinterpret_cast<f32x4*>(&qs[lr][c]) = load_f32x4(p.q + qr * D + c) * p.scale;
+  }
+  __syncthreads();
+  const uint32_t q_addr = lds_addr(&qs[n][KQ * q4]);
+
+  const int t0 = rb * RB / p.G, t1 = (min(R, rb * RB + RB) - 1) / p.G;
+  KeyTiles<16> tiles;
+  tiles.list(Pb, t0, p.cross ? 0 : t0 / p.L * p.L,
+             p.pass != 0 && !p.slot_pass ? t1 + 1 : min(p.T, (t1 / p.L + 1) * p.L), p.window, p.sinks);
+  const int n_pre = tiles.n_pre, nt = tiles.nt;
+  const float* kc = p.k_cache + (size_t)bg * p.C * D;
+  const float* vc = p.v_cache + (size_t)bg * p.C * D + d0;
+  const float* ks_ = p.k_slot + (size_t)bg * p.T * D;
+  const float* vs_ = p.v_slot + (size_t)bg * p.T * D + d0;
+
+  f32x4 oacc[NR][NOB];
+  float m[NR], l[NR];
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    m[r] = -INFINITY;
+    l[r] = 0.f;
+#pragma unroll
+    for (int ob = 0; ob < NOB; ++ob) oacc[r][ob] = f32x4{0.f, 0.f, 0.f, 0.f};
+  }
+
+  f32x4 kf[NKS];
+  uint32_t kcode[NKS / 2], kscale = 0;  // CODES: a prefix tile's codes, two pieces a word, and their scale
+  // K row n of tile i, clamped to the last valid key (its score is masked)
+  auto load_k = [&](int i) {
+    const bool pre = i < n_pre;
+    const int key0 = tiles.key0(i);
+    const int key = min(key0 + n, (pre ? Pb : p.T) - 1);
+    if constexpr (CODES) {
+      if (pre) {
+        const size_t at = (size_t)bg * p.C + key;
+        const uint32_t* src = reinterpret_cast<const uint32_t*>(p.k_cache) + at * (D / 8) + q4 * (D / 32);
+#pragma unroll
+        for (int e = 0; e < NKS / 2; ++e) kcode[e] = src[e];
+        kscale = p.k_scale[at * (D / 32) + q4 * (D / 4) / 32];
+        return;
+      }
+    }
+    const float* src = (pre ? kc : ks_) + (size_t)key * D + KQ * q4;
+#pragma unroll
+    for (int ks = 0; ks < NKS; ++ks) kf[ks] = load_f32x4(src + KP * ks);
+  };
+  // four elements of V row `key` from d on (d0: the first taken by this workgroup);
+  // `row`: the same row of a cache that is not in 4 bits
+  auto load_v4 = [&](bool pre, int key, int d, const float* row) __attribute__((always_inline)) {
+    if constexpr (CODES) {
+      if (pre) {
+        const size_t at = (size_t)bg * p.C + key;
+        const uint32_t c = reinterpret_cast<const uint16_t*>(p.v_cache)[at * (D / 4) + (d0 + d) / 4];
+        return q4_f32x4(c, q4_scale(p.v_scale[at * (D / 32) + (d0 + d) / 32]));
+      }
+    }
+    return load_f32x4(row + d);
+  };
+
+  if (wave < nt) load_k(wave);
+  for (int i = wave; i < nt; i += NW) {
+    const bool pre = i < n_pre;
+    const int key0 = tiles.key0(i);
+    const int last = (pre ? Pb : p.T) - 1;
+    const float* vsrc = pre ? vc : vs_;
+    f32x4 vf[4][NC];  // V rows 4 * q4 + v, elements 64 * c + 4 * n + e
+#pragma unroll
+    for (int v = 0; v < 4; ++v)
+#pragma unroll
+      for (int c = 0; c < NC; ++c)
+        vf[v][c] = load_v4(pre, min(key0 + 4 * q4 + v, last), 64 * c + 4 * n,
+                           vsrc + (size_t)min(key0 + 4 * q4 + v, last) * D);
+    if constexpr (CODES) {
+      if (pre) {
+#pragma unroll
+        for (int ks = 0; ks < NKS; ++ks) kf[ks] = q4_f32x4(kcode[ks / 2] >> (16 * (ks & 1)), q4_scale(kscale));
+      }
+    }
+
+    f32x4 s[NR];  // scores of keys 4 * q4 + v
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      f32x4 s0{0.f, 0.f, 0.f, 0.f}, s1{0.f, 0.f, 0.f, 0.f};  // two chains
+      // query fragments come from LDS for each tile (in registers they would
+      // not leave room for the output and the key and value pieces in flight)
+      bf16x8 qf[NKS];
+      const uint32_t qa = q_addr + r * 16 * QSTR * 4;
+      qf[0] = lds_read_b128<0>(qa);
+      qf[1] = lds_read_b128<4 * KP>(qa);
+      qf[2] = lds_read_b128<8 * KP>(qa);
+      qf[3] = lds_read_b128<12 * KP>(qa);
+      if constexpr (NKS == 8) {
+        qf[4] = lds_read_b128<16 * KP>(qa);
+        qf[5] = lds_read_b128<20 * KP>(qa);
+        qf[6] = lds_read_b128<24 * KP>(qa);
+        qf[7] = lds_read_b128<28 * KP>(qa);
+      }
+      lds_wait<0>();
+#pragma unroll
+      for (int ks = 0; ks < NKS; ++ks) lds_tie(qf[ks]);
+#pragma unroll
+      for (int ks = 0; ks < NKS; ks += 2) {
+        const f32x4 qa4 = __builtin_bit_cast(f32x4, qf[ks]), qb4 = __builtin_bit_cast(f32x4, qf[ks + 1]);
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          s0 = mfma16x16x4_f32(kf[ks][e], qa4[e], s0);
+          s1 = mfma16x16x4_f32(kf[ks + 1][e], qb4[e], s1);
+        }
+      }
+      s[r] = s0 + s1;
+    }
+    // the next tile's keys take the registers of this one's and arrive during
+    // the softmax and the PV products
+    __builtin_amdgcn_sched_barrier(0);
+    if (i + NW < nt) load_k(i + NW);
+    __builtin_amdgcn_sched_barrier(0);
+    // not every key shown, and a sink or inside the last token's window
+    const bool masked = !pre || key0 + 16 > Pb || !(key0 + 16 <= p.sinks || key0 > Pb + t1 - p.window);
+    auto visible = [&](int r, int key) {
+      const bool shown = pre ? key < Pb : key >= vis_lo[r] && key < vis_hi[r];
+      return shown && (key < p.sinks - (pre ? 0 : Pb) || key >= win_lo[r] + (pre ? Pb : 0));
+    };
+#pragma unroll
+    for (int r = 0; r < NR; ++r) {
+      if (masked) {
+#pragma unroll
+        for (int v = 0; v < 4; ++v)
+          if (!visible(r, key0 + 4 * q4 + v)) s[r][v] = -INFINITY;
+      }
+      float mt = max3f(max3f(s[r][0], s[r][1], s[r][2]), s[r][3], s[r][3]);
+      mt = fmaxf(mt, __shfl_xor(mt, 16));
+      mt = fmaxf(mt, __shfl_xor(mt, 32));
+      const float m_new = fmaxf(m[r], mt);
+      if (__any(m_new > m[r])) {
+        const float c = m[r] == -INFINITY ? 0.f : expf(m[r] - m_new);
+        l[r] *= c;
+#pragma unroll
+        for (int ob = 0; ob < NOB; ++ob)
+#pragma unroll
+          for (int v = 0; v < 4; ++v) oacc[r][ob][v] *= c;
+        m[r] = m_new;
+      }
+#pragma unroll
+      for (int v = 0; v < 4; ++v) {
+        s[r][v] = s[r][v] == -INFINITY ? 0.f : expf(s[r][v] - m_new);
+        l[r] += s[r][v];
+      }
+    }
+    // A value a row does not see must not reach it, and 0 * inf or 0 * NaN
+    // would: such tiles (masked, with a value that is not finite) are summed
+    // key by key over the visible keys only.
+    bool bad = false;
+    if (masked) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+#pragma unroll
+        for (int c = 0; c < NC; ++c)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) bad = bad || !(fabsf(vf[v][c][e]) < INFINITY);
+      bad = __any(bad);
+    }
+    if (!bad) {
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+#pragma unroll
+        for (int r = 0; r < NR; ++r)
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+              oacc[r][4 * c + e] = mfma16x16x4_f32(vf[v][c][e], s[r][v], oacc[r][4 * c + e]);
+    } else {
+#pragma unroll
+      for (int r = 0; r < NR; ++r)
+#pragma unroll 1
+        for (int j = 0; j < 16; ++j) {
+          const float pj = __shfl(j & 2 ? (j & 1 ? s[r][3] : s[r][2]) : (j & 1 ? s[r][1] : s[r][0]), 16 * (j >> 2) + n);
+          if (!visible(r, key0 + j)) continue;
+          const float* vrow = vsrc + (size_t)min(key0 + j, last) * D;
+#pragma unroll
+          for (int c = 0; c < NC; ++c)
+#pragma unroll
+            for (int v = 0; v < 4; ++v) {
+              const f32x4 vv = load_v4(pre, min(key0 + j, last), 16 * q4 + 64 * c + 4 * v, vrow);
+#pragma unroll
+              for (int e = 0; e < 4; ++e) oacc[r][4 * c + e][v] = fmaf(pj, vv[e], oacc[r][4 * c + e][v]);
+              __builtin_amdgcn_sched_barrier(0);
+            }
+        }
+    }
+  }
+
+  // ---- merge of the waves' partials, in wave order
+#pragma unroll
+  for (int r = 0; r < NR; ++r) {
+    l[r] += __shfl_xor(l[r], 16);
+    l[r] += __shfl_xor(l[r], 32);
+    const int lr = 16 * r + n;
+    if (q4 == 0) {
+      part_m[wave][lr] = m[r];
+      part_l[wave][lr] = l[r];
+    }
+    // oacc[4 * c + e][v] is element 64 * c + 16 * q4 + 4 * v + e of the row
+#pragma unroll
+    for (int c = 0; c < NC; ++c)
+#pragma unroll
+      for (int v = 0; v < 4; ++v)
+        *reinterpret_cast<f32x4*>(&part_o[wave][lr][64 * c + 16 * q4 + 4 * v]) =
+            f32x4{oacc[r][4 * c][v], oacc[r][4 * c + 1][v], oacc[r][4 * c + 2][v], oacc[r][4 * c + 3][v]};
+  }
+  __syncthreads();
+  for (int x = threadIdx.x; x < RB * (DO / 4); x += NW * 64) {
+    const int lr = x / (DO / 4), c = 4 * (x % (DO / 4));
+    const int row = rb * RB + lr;
+    if (row >= R) break;
+    float mx = part_m[0][lr];
+#pragma unroll
+    for (int i = 1; i < NW; ++i) mx = fmaxf(mx, part_m[i][lr]);
+    float lt = 0.f;
+    f32x4 o{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      const float pm = part_m[i][lr], pl = part_l[i][lr];
+      if (pm == -INFINITY && pl == 0.f) continue;  // a wave without a visible key of this row
+      const float sc = expf(pm - mx);
+      lt += sc * pl;
+      o += sc * *reinterpret_cast<const f32x4*>(&part_o[i][lr][c]);
+    }
+    const size_t grow = (size_t)bg * R + (size_t)(row % p.G) * p.T + row / p.G;
+    store_f32x4(p.out + grow * D + d0 + c, o / lt);
+    if (p.lse && d0 + c == 0) p.lse[grow] = mx + logf(lt);
+  }
+}
+
+// ------------------------------------------------------------------ launchers
+
+template <int D, bool CODES>
+void launch_view_as(const ViewParams& all, hipStream_t stream) {
+  for_each_view_launch(all, [&](const ViewParams& p) {
+    if (p.rows_per_block == kAttnWideRowsPerBlock) {
+      slot_view_bf16_kernel<D, 8, CODES, 1><<<dim3(8 * p.per_xcd), dim3(512), 0, stream>>>(p);
+    } else if (p.key_groups == 2) {
+      slot_view_bf16_kernel<D, 4, CODES, 2><<<dim3(8 * p.per_xcd), dim3(512), 0, stream>>>(p);
+    } else {
+      slot_view_bf16_kernel<D, 4, CODES, 1><<<dim3(8 * p.per_xcd), dim3(256), 0, stream>>>(p);
+    }
+  });
+}
+
+hipError_t launch_slot_view_bf16(const ViewParams& p, int head_dim, bool codes, hipStream_t stream) {
+  if (codes) {
+    head_dim == 128 ? launch_view_as<128, true>(p, stream) : launch_view_as<64, true>(p, stream);
+  } else {
+    head_dim == 128 ? launch_view_as<128, false>(p, stream) : launch_view_as<64, false>(p, stream);
+  }
+  const hipError_t e = hipGetLastError();
+  return e != hipSuccess || p.n_split == 1 ? e : launch_slot_attn_merge(p, head_dim, stream);
+}
+
+template <bool CODES, int D, int NR, int DS, int NW>
+void launch_view_f32_as(ViewParams32 p, int blocks, hipStream_t stream) {
+  const int64_t items = (int64_t)DS * blocks;
+  for (int64_t i = 0; i < items; i += kAttnMaxGrid) {
+    p.item0 = (int)i;
+    const int n = (int)std::min<int64_t>(items - i, kAttnMaxGrid);
+    slot_view_f32_kernel<D, NR, DS, NW, CODES><<<dim3(8 * ((n + 7) / 8)), dim3(NW * 64), 0, stream>>>(p);
+  }
+}
+
+template <bool CODES, int NR>
+void launch_view_f32_rows(const ViewParams32& p, int head_dim, int n_rb, hipStream_t stream) {
+  constexpr int NW = kAttnF32Waves;
+  const int blocks = p.B * p.Hkv * n_rb;
+  if (head_dim == 64) {
+    launch_view_f32_as<CODES, 64, NR, 1, NW>(p, blocks, stream);
+  } else if (NR == 1 && attn_f32_row_parts(head_dim, 16, blocks) == 2) {
+    launch_view_f32_as<CODES, 128, 1, 2, NW>(p, blocks, stream);
+  } else {
+    launch_view_f32_as<CODES, 128, NR, 1, NW>(p, blocks, stream);
+  }
+}
+
+// The choices of launch_slot_attn_f32, by the keys that a row block sees at most.
+template <bool CODES>
+hipError_t launch_view_f32(const ViewParams32& p, int head_dim, hipStream_t stream) {
+  const int64_t prefix = std::min<int64_t>(p.P, (int64_t)p.window + p.sinks);
+  const int R = p.G * p.T, rows = attn_f32_rows_per_block(p.B * (int64_t)p.Hkv, R, prefix + p.T);
+  if (attn_f32_one_wave(p.B * (int64_t)p.Hkv, R, attn_f32_keys_seen(prefix, p.T, p.L, p.cross))) {
+    const int blocks = p.B * p.Hkv * ((R + 15) / 16);
+    if (head_dim == 64) {
+      launch_view_f32_as<CODES, 64, 1, 1, 1>(p, blocks, stream);
+    } else {
+      launch_view_f32_as<CODES, 128, 1, 1, 1>(p, blocks, stream);
+    }
+    return hipGetLastError();
+  }
+  // 4-bit keys are read at an eighth of the bytes and stay with 16 rows (32 rows and
+  // the codes on their way do not fit the registers at D = 128)
+  if constexpr (!CODES) {
+    if (rows == 32) {
+      launch_view_f32_rows<CODES, 2>(p, head_dim, (R + 31) / 32, stream);
+      return hipGetLastError();
+    }
+  }
+  launch_view_f32_rows<CODES, 1>(p, head_dim, (R + 15) / 16, stream);
+  return hipGetLastError();
+}
+
+hipError_t launch_slot_view_f32(const ViewParams32& p, int head_dim, bool codes, hipStream_t stream) {
+  return codes ? launch_view_f32<true>(p, head_dim, stream) : launch_view_f32<false>(p, head_dim, stream);
+}
+
+}  // namespace zarya
