@@ -564,7 +564,8 @@ zarya_status zarya_slot_attn_q4_workspace_size(const zarya_slot_attn_desc* desc,
 
 /*
  * The cache arrays may be NULL only when P == 0.  q, the codes, the slot K/V, out
- * and the workspace must be 16-byte aligned.  The rest as zarya_slot_attn_window.
+ * and the workspace must be 16-byte aligned, the scales to a row of them (D/32
+ * bytes).  The rest as zarya_slot_attn_window.
  */
 zarya_status zarya_slot_attn_q4(const zarya_slot_attn_desc* desc, const zarya_attn_window* window, const void* q,
                                 const uint8_t* k_codes, const uint8_t* k_scales, const uint8_t* v_codes,

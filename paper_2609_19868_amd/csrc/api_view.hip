@@ -153,6 +153,9 @@ zarya_status run_view(const zarya_slot_attn_desc* d, const zarya_attn_window* w,
     return fail(ZARYA_ERR_INVALID_ARGUMENT, "the cache arrays are required when prefix_len > 0");
   if (!aligned16({q, k_cache, v_cache, k_slot, v_slot, out, workspace}))
     return fail(ZARYA_ERR_INVALID_ARGUMENT, "q, the caches, the slot K/V, out and the workspace must be 16-byte aligned");
+  const uintptr_t scales = reinterpret_cast<uintptr_t>(k_scale) | reinterpret_cast<uintptr_t>(v_scale);
+  if (scales % (d->head_dim / 32) != 0)
+    return fail(ZARYA_ERR_INVALID_ARGUMENT, "the scales must be aligned to a row of them (%d bytes)", d->head_dim / 32);
   const ViewPlan pl = plan_view(d, w, codes);
   if (workspace_bytes < pl.ws_bytes)
     return fail(ZARYA_ERR_WORKSPACE_TOO_SMALL, "workspace of %zu bytes is below the %zu required", workspace_bytes,

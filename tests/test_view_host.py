@@ -110,8 +110,11 @@ def test_attention_rejects_missing_misaligned_and_short_buffers():
         assert _window(_desc(), (5, 0), {i: odd}) == INV
     for i in (0, 1, 2, 3, 4, 5, 6, 9):
         assert _q4(_desc(), None, {i: None}) == INV
-        if i not in (2, 4):  # scales are read by the byte
+        if i not in (2, 4):
             assert _q4(_desc(), None, {i: odd}) == INV
+    for i in (2, 4):  # a row of scales is D/32 bytes
+        for D, by in ((128, 1), (128, 2), (64, 1)):
+            assert _q4(_desc(head_dim=D), None, {i: ctypes.c_void_p(4096 + by)}) == INV
     need = _lib.slot_attn_q4_workspace_size(_desc())
     assert need > 0
     assert _q4(_desc(), None, ws_bytes=need - 1) == WS
