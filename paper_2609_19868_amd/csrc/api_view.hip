@@ -36,18 +36,21 @@ zarya_status check_view(const zarya_slot_attn_desc* d, const zarya_attn_window* 
 
 // Splits of blocks of 128 or 256 rows.  `base` blocks with `tiles` key tiles each, of
 // which a workgroup takes `tile_ns` a tile, are split no further than to a workgroup
-// a unit; a split costs the merge's launch, and its partials' way to memory and back.
+// a unit; a split costs the merge's launch, and its partials' way to memory and back:
+// tiles * tile_ns / ns + merge + ns * partials.  Compared without rounding, as
+// fractions over the rate times ns: then more tiles never take fewer splits.
 int best_splits(int64_t base, int64_t tiles, int64_t tile_ns, int64_t partial_bytes, int64_t* cost) {
   const int64_t most = std::max<int64_t>(1, std::min<int64_t>({64, tiles, kAttnTargetWGs / base}));
   int best = 1;
-  *cost = tiles * tile_ns * ((base + kAttnTargetWGs - 1) / kAttnTargetWGs);
+  int64_t num = tiles * tile_ns * ((base + kAttnTargetWGs - 1) / kAttnTargetWGs) * kViewPartialBytesPerNs;
   for (int ns = 2; ns <= most; ++ns) {
-    const int64_t c = (tiles * tile_ns + ns - 1) / ns + kViewMergeNs + ns * partial_bytes / kViewPartialBytesPerNs;
-    if (c < *cost) {
-      *cost = c;
+    const int64_t c = (tiles * tile_ns + ns * kViewMergeNs) * kViewPartialBytesPerNs + ns * ns * partial_bytes;
+    if (c * best < num * ns) {
+      num = c;
       best = ns;
     }
   }
+  *cost = num / (best * kViewPartialBytesPerNs);
   return best;
 }
 

@@ -127,6 +127,17 @@ def test_attention_rejects_missing_misaligned_and_short_buffers():
     assert _lib.slot_attn_window_workspace_size(d, _lib.AttnWindow(10, 4)) == 0
 
 
+@pytest.mark.parametrize("shape", [
+    dict(batch=1, n_q_heads=4, n_kv_heads=1, n_slots=2, slot_len=16, head_dim=64, cross_slot=0),
+    dict(batch=1, n_q_heads=20, n_kv_heads=4, n_slots=2, slot_len=8, head_dim=128, cross_slot=1),
+])
+def test_workspace_of_the_longest_prefix_serves_all(shape):
+    """At every length: where two numbers of splits cost the same to a nanosecond, a
+    longer prefix must not fall back to the smaller one."""
+    sizes = [_lib.slot_attn_q4_workspace_size(_desc(prefix_len=n, kv_capacity=20000, **shape)) for n in range(0, 20000)]
+    assert sizes[-1] > 0 and all(a <= b for a, b in zip(sizes, sizes[1:]))
+
+
 @pytest.mark.parametrize("bad,code", [
     (dict(batch=0), INV), (dict(n_kv_heads=0), INV), (dict(n_rows=-1), INV), (dict(kv_capacity=-1, n_rows=0), INV),
     (dict(dtype=5), INV), (dict(n_rows=4097), INV), (dict(head_dim=80), UNS),
