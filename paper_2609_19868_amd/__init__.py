@@ -302,10 +302,10 @@ def slot_attn_q4(q, cache, k_slot, v_slot, n_slots, slot_len, pass_=PASS_DIFFUSI
     B, Hq, T, D = q.shape
     dev, dt = q.device, q.dtype
     Hkv = k_slot.shape[1]
-    desc = slot_attn_desc(q, cache.k, k_slot, n_slots, slot_len, pass_, cross_slot, prefix_len, softmax_scale,
+    shape = _need_q4(cache, dev)
+    desc = slot_attn_desc(q, cache[0], k_slot, n_slots, slot_len, pass_, cross_slot, prefix_len, softmax_scale,
                           prefix_splits)
     out, lse = _attn_tensors(q, k_slot, v_slot, n_slots, slot_pass, prefix_lens, out, lse, want_lse)
-    shape = _need_q4(cache, dev)
     if shape != (B, Hkv, desc.kv_capacity, D):
         raise ValueError(f"cache: expected batch, heads and head size {(B, Hkv, D)}, got {(shape[0], shape[1], shape[3])}")
     win = _window(window, sinks)
@@ -540,7 +540,7 @@ def kv_dequantize(cache, n_rows=None, dtype=torch.bfloat16, lens=None, out=None)
     lens: int32 [B] or None; rows from lens[b] on are left as they are in ``out``
     (unset where the call makes its own).  Returns (k, v) [B,Hkv,n_rows,D].
     """
-    dev = cache.k.device
+    dev = cache[0].device
     B, Hkv, C, D = _need_q4(cache, dev)
     N = C if n_rows is None else int(n_rows)
     if dtype not in _DT:

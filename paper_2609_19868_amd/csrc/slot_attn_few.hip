@@ -75,6 +75,7 @@ struct FewRaw<D, true> {
   uint32_t ks[2];
   uint32_t v[8];        // D/16 codes of each of eight keys
   uint32_t vs[D / 16];  // the eight keys' scales, D/32 bytes a key
+  bf16x8 ring_vs[2];    // the same as the ring's reads leave them
 };
 
 template <int D>
@@ -228,15 +229,6 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
 
   // scores, online softmax and value products of one tile
   auto compute = [&](auto& raw, bool pre, int key0, auto ring) __attribute__((always_inline)) {
-    if constexpr (decltype(ring)::value) {
-      lds_wait<10>();  // K's codes and scales
-#pragma unroll
-      for (int t = 0; t < 2; ++t) {
-        lds_tie(raw.ks[t]);
-#pragma unroll
-        for (int e = 0; e < D / 32; ++e) lds_tie(raw.k[t][e]);
-      }
-    }
     constexpr bool Codes = std::is_same_v<std::decay_t<decltype(raw)>, FewRaw<D, true>>;
     f32x4 s[NT][2];
 #pragma unroll
@@ -279,7 +271,7 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
       mt = max3f(max3f(mt, s[r][1][1], s[r][1][2]), s[r][1][3], s[r][1][3]);
       mt = max_xor32(max_xor16(mt));
       const float m_new = fmaxf(m[r], mt);
-      // as in attn_bf16_body: sums are rescaled only once a maximum has grown by 2^8
+      // as in slot_view_bf16_kernel: sums are rescaled only once a maximum has grown by 2^8
       if (__any((m_new - m[r]) * c2 > kRescaleLog2)) {
         const float alpha = fast_exp2((m[r] - m_new) * c2);
         l[r] *= alpha;
@@ -303,9 +295,15 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
     if constexpr (decltype(ring)::value) {
       lds_wait<0>();
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        lds_tie(raw.v[j]);
-        lds_tie(raw.vs[j]);
+      for (int j = 0; j < 8; ++j) lds_tie(raw.v[j]);
+#pragma unroll
+      for (int t = 0; t < 2; ++t) {
+        lds_tie(raw.ring_vs[t]);
+        const uint4 w = __builtin_bit_cast(uint4, raw.ring_vs[t]);
+        raw.vs[4 * t] = w.x;
+        raw.vs[4 * t + 1] = w.y;
+        raw.vs[4 * t + 2] = w.z;
+        raw.vs[4 * t + 3] = w.w;
       }
     }
     // element pair (2e, 2e + 1) of the lane's part of key j's V row, as packed bf16
@@ -414,18 +412,9 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
       }
       const uint32_t at = lane0 + slot * TILE;
       FewRaw<D, true> raw;
-      auto quarter = [&](uint32_t (&dst)[4], const bf16x8& x) __attribute__((always_inline)) {
-        const uint4 w = __builtin_bit_cast(uint4, x);
-        dst[0] = w.x;
-        dst[1] = w.y;
-        dst[2] = w.z;
-        dst[3] = w.w;
-      };
-      const bf16x8 k0 = lds_read_b128<0>(at + k_at), k1 = lds_read_b128<1024>(at + k_at);
+      bf16x8 k[2] = {lds_read_b128<0>(at + k_at), lds_read_b128<1024>(at + k_at)};
       raw.ks[0] = lds_read_u8<0>(at + ks_at);
       raw.ks[1] = lds_read_u8<4 * (D / 32)>(at + ks_at);
-      quarter(raw.k[0], k0);
-      quarter(raw.k[1], k1);
       uint32_t va[4];
 #pragma unroll
       for (int j = 0; j < 4; ++j) va[j] = at + v_at + 16 * ((n >> 2) ^ j);
@@ -437,11 +426,19 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
       raw.v[5] = lds_read_b32<20 * (D / 2)>(va[1]);
       raw.v[6] = lds_read_b32<24 * (D / 2)>(va[2]);
       raw.v[7] = lds_read_b32<28 * (D / 2)>(va[3]);
-      const bf16x8 s0 = lds_read_b128<0>(at + vs_at), s1 = lds_read_b128<16>(at + vs_at);
-      const uint4 w0 = __builtin_bit_cast(uint4, s0), w1 = __builtin_bit_cast(uint4, s1);
-      const uint32_t w[8] = {w0.x, w0.y, w0.z, w0.w, w1.x, w1.y, w1.z, w1.w};
+      raw.ring_vs[0] = lds_read_b128<0>(at + vs_at);
+      raw.ring_vs[1] = lds_read_b128<16>(at + vs_at);
+      lds_wait<10>();  // K's codes and scales; V's are waited for in `compute`
 #pragma unroll
-      for (int j = 0; j < 8; ++j) raw.vs[j] = w[j];
+      for (int t = 0; t < 2; ++t) {
+        lds_tie(k[t]);
+        lds_tie(raw.ks[t]);
+        const uint4 w = __builtin_bit_cast(uint4, k[t]);
+        raw.k[t][0] = w.x;
+        raw.k[t][1] = w.y;
+        raw.k[t][2] = w.z;
+        raw.k[t][3] = w.w;
+      }
       compute(raw, true, tiles.key0(i), yes);
       slot = slot == RING - 1 ? 0 : slot + 1;
     }
@@ -484,17 +481,20 @@ __global__ __launch_bounds__(NW * 64) __attribute__((amdgpu_waves_per_eu(2))) vo
     compute(raw, pre, tiles.key0(i), no);
   }
 
-  // ---- values that are not finite: as in attn_bf16_body, the wave's sums once
+  // ---- values that are not finite: as in slot_view_bf16_kernel, the wave's sums once
   // more, key by key over the visible ones
   {
-    float z = 0.f;
+    bool again = false;
 #pragma unroll
-    for (int r = 0; r < NT; ++r)
+    for (int r = 0; r < NT; ++r) {
+      float z = 0.f;
 #pragma unroll
       for (int ob = 0; ob < NOB; ++ob)
 #pragma unroll
         for (int v = 0; v < 4; ++v) z = fmaf(oacc[r][ob][v], 0.f, z);
-    if (__any(z != 0.f)) {
+      again |= z != 0.f && l[r] * 0.f == 0.f;
+    }
+    if (__any(again)) {
 #pragma unroll
       for (int r = 0; r < NT; ++r)
 #pragma unroll

@@ -461,13 +461,14 @@ __global__ __launch_bounds__(NWAVE * GRP * 64) __attribute__((amdgpu_waves_per_e
   // A value that is not finite has left its mark on the sums of every row whose
   // tile held it, seen or not (0 * inf).  Then the wave's sums are taken once
   // more, key by key over the visible ones (the maxima and the sums of the
-  // probabilities never saw the others).
+  // probabilities never saw the others).  Where those are no numbers either the row's
+  // result is none and there is nothing to take again.
   float z = 0.f;
 #pragma unroll
   for (int db = 0; db < NDB; ++db)
 #pragma unroll
     for (int v = 0; v < 16; ++v) z = fmaf(oacc[db][v], 0.f, z);
-  if (__any(row_ok && z != 0.f)) {
+  if (__any(row_ok && z != 0.f && l_run * 0.f == 0.f)) {
 #pragma unroll
     for (int db = 0; db < NDB; ++db) oacc[db] = f32x16{};
     // eight elements from d on of a row of K (which = 0) or V
