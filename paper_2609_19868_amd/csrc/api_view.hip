@@ -4,7 +4,7 @@
 #include <algorithm>
 
 #include "host.hpp"
-#include "kernels.hpp"
+#include "view.hpp"
 #include "zarya.h"
 
 using namespace zarya;

@@ -49,20 +49,6 @@ struct AttnParams32 {
   int item0;  // first work item of this launch (set by the launcher)
 };
 
-// The same over a bounded view of the prefix (attn_view.hpp).
-template <class Params>
-struct ViewOf : Params {
-  const uint8_t* k_scale;  // [B, Hkv, C, D/32] of 4-bit caches
-  const uint8_t* v_scale;
-  int window;  // >= 1 (INT32_MAX: none)
-  int sinks;
-};
-struct ViewParams : ViewOf<AttnParams> {
-  int item0;       // first work item of this launch (set by the launcher)
-  int key_groups;  // groups of waves that share a block's tiles (blocks of 128 rows: 1 or 2)
-};
-using ViewParams32 = ViewOf<AttnParams32>;
-
 // LM-head confidence.  Partials are per (vocab group, row): m = max logit,
 // s = sum of exp(logit - m), idx = lowest id at the max.
 struct ConfParams {
@@ -153,35 +139,6 @@ struct AppendParams {
   void* v_cache;
 };
 
-// The 4-bit cache: codes [B, Hkv, C, D/2] and scale bytes [B, Hkv, C, D/32] of K and V.
-struct Q4CachePtrs {
-  uint8_t* k_codes;
-  uint8_t* k_scales;
-  uint8_t* v_codes;
-  uint8_t* v_scales;
-};
-
-struct KvQ4Params {
-  int B, Hkv, C, N, D;
-  int bf16;
-  void* k;  // [B, Hkv, N, D], only read when quantizing
-  void* v;
-  const int32_t* starts;  // [B] or null
-  const int32_t* lens;    // [B] or null
-  Q4CachePtrs cache;      // only read when dequantizing
-};
-
-struct AppendQ4Params : AppendParams {
-  int D, bf16;
-  Q4CachePtrs cache;  // instead of k_cache and v_cache
-  int copies, counts;  // this launch fills the cache; moves the prefix lengths (set by the launcher)
-};
-// Pieces of eight elements, K's and V's of all draft tokens of a row, that one
-// workgroup takes, and beyond that each of several (8 heads, D = 128, a third of the
-// tokens accepted and all: 64 tokens in one launch 9.0 and 11.3 us, in two 9.5 and
-// 10.1; 128 9.3 and 18.7, 9.1 and 10.1; 4096, all, 497 and 20.5).
-constexpr int64_t kAppendQ4OneWG = 16384, kAppendQ4PartPieces = 4096;
-
 // Mode A reveal: one workgroup per batch row sorts the row's N keys in LDS.
 struct RevealParams {
   int B, N, NP;  // NP = N rounded up to a power of two (>= 2)
@@ -213,37 +170,6 @@ constexpr int kAttnMaxGrid = 1 << 20;
 constexpr int kAttnRowsPerBlock = 128;      // four waves
 constexpr int kAttnWideRowsPerBlock = 256;  // eight waves: every K/V tile staged once for 256 rows
 constexpr int kAttnTargetWGs = 256;         // workgroups the bf16 planner splits the prefix for: one a compute unit
-// Bounded views, blocks of 16 or 32 rows: up to this many rows of a GQA group.  In 4
-// bits 64: 16/8 heads, 4096 keys, 48 rows x 1 and 16 sequences 12.9 and 34.2 us, 15.4
-// and 39.5 with 128-row blocks; 64 x 2048 keys, 64 rows 62 and 72, but 96 rows 88 and
-// 79.  In bf16 32: 16 sequences, 32 rows 58.7 us, 48 rows 73.8 and 60.8.
-constexpr int kViewFewRows = 32;
-constexpr int kViewFewRowsCodes = 64;
-// Their splits: up to 512 workgroups (two of four waves a unit in bf16, three in 4
-// bits) while each keeps three 32-key tiles, and no more than 32 (one sequence, one
-// token: 512 bf16 keys 6.7 us with 6 splits, 9.2 with 1; 16384 4-bit keys 11.5 with 32,
-// 13.3 with 16, 12.7 with 64); and where each keeps 64 tiles up to 2048 workgroups, so
-// that rows of different lengths even out (64 sequences of 4096 to 8191 4-bit keys 86
-// us with 4 splits, 102 with 1; all of 8191 109 and 118).
-constexpr int kViewFewTargetWGs = 512, kViewFewMinTiles = 3;
-constexpr int kViewFewBalanceWGs = 2048, kViewFewBalanceTiles = 64;
-// Blocks of 128 or 256 rows: nanoseconds of a 64-key tile of a workgroup (D = 128, fitted
-// to the 4B heads' shapes over 512 to 16384 keys).  128-row blocks are taken by two
-// groups of four waves that share the tiles, where there are no more blocks than
-// units; more of them run two a unit.  8 sequences, 512 rows a group, 256-row blocks in
-// two splits and 128-row ones without: 4-bit keys, a window of 1024 37.3 and 27.1 us,
-// 4096 79.7 and 73.7, 8192 137.2 and 136.2, 16384 keys 252.9 and 263.3; bf16 37.5 and
-// 28.4, 83.3 and 81.6, 150.7 and 153.0, 279.3 and 295.4.
-struct ViewTileNs {
-  int64_t wide, narrow, narrow_pair;
-};
-constexpr ViewTileNs view_tile_ns(bool codes, int head_dim) {
-  const ViewTileNs t = codes ? ViewTileNs{1800, 1000, 2200} : ViewTileNs{2050, 1120, 2250};
-  return head_dim == 128 ? t : ViewTileNs{t.wide * 5 / 8, t.narrow * 5 / 8, t.narrow_pair * 5 / 8};
-}
-// A merge's launch, and the rate of the partials (4 sequences, 512 rows a group, window
-// 512: 26.9 us with two splits, 18.5 with one; 2048 36.7 and 39.8).
-constexpr int64_t kViewMergeNs = 4000, kViewPartialBytesPerNs = 2600;
 // float32 path: query rows per workgroup.  32 rows read each key half as often
 // as 16; 16 rows make twice as many workgroups, which pays where 32 leave
 // compute units idle (16/8 heads x 64 tokens, D = 128, 16 and 32 rows: 2048 keys,
@@ -316,35 +242,14 @@ constexpr int conf_tile_rows(int n_rows) { return n_rows <= kConfSmallMaxRows ? 
 constexpr int kConfF32MinIds = 128;
 constexpr int conf_f32_tile_rows(int n_rows) { return n_rows <= 32 ? 32 : 64; }
 
-// launch(p) over the work items of p in grids of at most kAttnMaxGrid workgroups
-// (heavy_first takes one grid; the host asks for it only where that holds them).
-template <class Launch>
-void for_each_view_launch(ViewParams p, Launch&& launch) {
-  const int n = p.n_items;
-  for (int i = 0; i < n; i += p.n_items) {
-    p.item0 = i;
-    p.n_items = n - i < kAttnMaxGrid ? n - i : kAttnMaxGrid;
-    p.per_xcd = (p.n_items + 7) / 8;
-    launch(p);
-  }
-}
-
 hipError_t launch_slot_attn_bf16(const AttnParams& p, int head_dim, hipStream_t stream);
 hipError_t launch_slot_attn_f32(const AttnParams32& p, int head_dim, hipStream_t stream);
-hipError_t launch_slot_attn_merge(const AttnParams& p, int head_dim, hipStream_t stream);  // of the prefix splits
-// `codes`: the caches hold 4-bit codes
-hipError_t launch_slot_view_bf16(const ViewParams& p, int head_dim, bool codes, hipStream_t stream);
-hipError_t launch_slot_view_few(const ViewParams& p, int head_dim, bool codes, hipStream_t stream);  // blocks of 16 or 32 rows
-hipError_t launch_slot_view_f32(const ViewParams32& p, int head_dim, bool codes, hipStream_t stream);
 hipError_t launch_slot_conf_bf16(const ConfParams& p, hipStream_t stream);
 hipError_t launch_slot_conf_f32(const ConfParams& p, hipStream_t stream);
 hipError_t launch_slot_conf_merge(const ConfMergeParams& p, hipStream_t stream);
 hipError_t launch_select_slots(const SelectParams& p, hipStream_t stream);
 hipError_t launch_verify_accept(const AcceptParams& p, hipStream_t stream);
 hipError_t launch_kv_append(const AppendParams& p, hipStream_t stream);
-hipError_t launch_kv_quantize(const KvQ4Params& p, hipStream_t stream);
-hipError_t launch_kv_dequantize(const KvQ4Params& p, hipStream_t stream);
-hipError_t launch_kv_append_q4(const AppendQ4Params& p, hipStream_t stream);
 hipError_t launch_mdm_reveal(const RevealParams& p, hipStream_t stream);
 
 }  // namespace zarya

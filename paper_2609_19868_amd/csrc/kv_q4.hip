@@ -12,8 +12,8 @@
 
 #include "attn_view.hpp"
 #include "common.hpp"
-#include "kernels.hpp"
 #include "kv_q4.hpp"
+#include "view.hpp"
 
 namespace zarya {
 

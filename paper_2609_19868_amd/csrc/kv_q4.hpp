@@ -3,7 +3,7 @@
 #pragma once
 
 #include "common.hpp"
-#include "kernels.hpp"
+#include "view.hpp"
 
 namespace zarya {
 

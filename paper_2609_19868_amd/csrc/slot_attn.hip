@@ -31,7 +31,7 @@
 #include <utility>
 
 #include "common.hpp"
-#include "kernels.hpp"
+#include "view.hpp"
 
 namespace zarya {
 

@@ -24,7 +24,7 @@
 
 #include "attn_view.hpp"
 #include "common.hpp"
-#include "kernels.hpp"
+#include "view.hpp"
 
 namespace zarya {
 

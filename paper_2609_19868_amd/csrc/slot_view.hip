@@ -20,7 +20,7 @@
 
 #include "attn_view.hpp"
 #include "common.hpp"
-#include "kernels.hpp"
+#include "view.hpp"
 
 namespace zarya {
 

@@ -6,7 +6,7 @@
 #include <cstring>
 #include <random>
 
-#include "kernels.hpp"
+#include "view.hpp"
 #include "zarya.h"
 
 static int g_fail = 0, g_checks = 0, g_launches = 0, g_few = 0, g_split = 0;
